@@ -53,7 +53,10 @@ typedef enum {
   MUSTDROP_ERR_CUDA = 5,          /* a CUDA runtime call failed; see mustdrop_last_cuda_error */
   MUSTDROP_ERR_TIMEOUT = 6,       /* device status only: a bounded wait inside a kernel ran out */
   MUSTDROP_ERR_BAD_KEY_INDEX = 7, /* device status only: an index outside [0, n_vis) was ignored */
-  MUSTDROP_ERR_SCRATCH_LIMIT = 8  /* mustdrop_score_static: batch * n_heads * n_txt exceeds the built-in scratch */
+  MUSTDROP_ERR_SCRATCH_LIMIT = 8, /* mustdrop_score_static: batch * n_heads * n_txt exceeds the built-in scratch */
+  MUSTDROP_ERR_BAD_PAGE = 9,      /* device status only: a page id or slot outside the pool was ignored */
+  MUSTDROP_ERR_BAD_LENGTH = 10,   /* device status only: a sequence length or growth outside its limits was refused */
+  MUSTDROP_ERR_NO_PAGES = 11      /* device status only: too few free pages for a sequence, which did not grow */
 } mustdrop_status_t;
 
 typedef enum { MUSTDROP_MODE_BUDGET = 0, MUSTDROP_MODE_THRESHOLD = 1 } mustdrop_mode_t;
@@ -350,6 +353,114 @@ mustdrop_status_t mustdrop_spatial_merge(int32_t batch, int32_t grid, int32_t wi
 mustdrop_status_t mustdrop_key_set(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_tokens,
                                    int32_t key_max, const void *q_cls, const void *k, float *a_cls,
                                    float *mu_out, int32_t *key_idx, int32_t *key_cnt, void *cuda_stream);
+
+/*
+ * Decoding-stage cache in pages of 4-bit values (mustdrop_page_*).  After the pruning layers every
+ * layer and request holds another number of tokens (Sec. 3.4, 3.5), known on the GPU only
+ * (kept_cnt).  These calls keep all of them in one pool: mustdrop_page_tables gives tokens their
+ * places from lengths on the GPU, mustdrop_page_store quantises K / V rows into them,
+ * mustdrop_page_load reads them back, mustdrop_page_attend is the attention of the decoded tokens.
+ * (The paper has no counterpart; its cache policy decides WHICH tokens such a cache holds.)
+ *
+ * A SEQUENCE is one request's cache at one layer; callers number them as they like (layer * batch +
+ * request lets one layer's attention take a slice of the tables).  A PAGE holds `page` tokens of one
+ * sequence for all heads.  SLOT = page id * page + place inside the page.
+ *
+ * Values: the 32 consecutive channels of one token and head are a group with a scale s and a centre
+ * z, both bf16, and 4-bit codes c; a value is z + s (c - 8).  With m, M the group's least and
+ * greatest member: s = bf16((M/2 - m/2) / 7.5), z = bf16(m + 8 s), c = clamp(round((x - z) / s) + 8,
+ * 0, 15), each step one fp32 operation, ties to even; c = 8 where s = 0.  A group with an infinity
+ * or a NaN reads back as NaN.  (A value is off by at most s / 2, and by what rounding s and z moves.)
+ *
+ * Pool: n_pages x n_heads x (page / 16) chunks of 20 * head_dim bytes.  A chunk holds 16 tokens;
+ * token k of it has the row r(k) = k / 2 + 8 (k mod 2).  With G = head_dim / 32, bytes in this order:
+ *   [16 r][4 t][G g][4 b]                      K codes: channel 32 g + 8 t + 2 b low half of the byte, the next one high
+ *   [head_dim/64 a][8 i][4 t][2 h][2 e][4 b]   V codes of token 4 t + b: channel 32 (2 a + h) + 4 i + 2 e low, the next high
+ *   [16 r][G s, G z] bf16                      K scales and centres
+ *   [16 r][G] bf16                             V scales
+ *   [G][16 r] bf16                             V centres
+ * (the order in which the attention kernel's matrix instructions take their operands).  The pool
+ * needs no initial value: bytes of tokens that were never stored are never used.
+ *
+ * All pointers are device memory; q, k, v, out, pool and workspace are 16-byte aligned, int32 arrays
+ * 4-byte aligned.  The workspace (mustdrop_page_workspace_bytes, zeroed once) starts with the status
+ * word (int32 code, int32 detail); calls that may overlap on the GPU need workspaces of their own.
+ * Device-detected conditions (MUSTDROP_ERR_BAD_PAGE, _BAD_LENGTH, _NO_PAGES) are recorded there and
+ * never trap; detail is the sequence (mustdrop_page_attend, bad page: the id).
+ */
+typedef struct {
+  int32_t n_seq;      /* sequences of the call, 1..65535 (mustdrop_page_attend: ..4096) */
+  int32_t n_heads;    /* K / V heads, 1..65535 */
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t page;       /* tokens per page: 16, 32, 64 or 128 */
+  int32_t n_pages;    /* pages of the pool; n_pages * page < 2^31 */
+  int32_t max_pages;  /* entries per row of page_table; max_pages * page < 2^31 */
+  int32_t rows;       /* tables, store, load: rows per sequence of slots and k / v */
+  int32_t q_heads;    /* attend: query heads, a multiple of n_heads; heads h * q_heads / n_heads .. share K / V head h */
+  int32_t n_q;        /* attend: query tokens per sequence, 1..128 */
+  int32_t causal;     /* attend: 1: query token t sees keys 0 .. len - n_q + t (the queries are the last n_q tokens); 0: all len keys */
+  float   scale;      /* attend: logit scale; 0 => 1/sqrt(head_dim) */
+  int32_t flags;      /* must be 0 */
+  /* Strides in ELEMENTS (bf16); 0 => contiguous; each a multiple of 8.  Rows of head_dim elements are contiguous. */
+  int64_t k_stride_s, k_stride_h, k_stride_r;   /* store: k [n_seq, n_heads, rows, head_dim] */
+  int64_t v_stride_s, v_stride_h, v_stride_r;   /* store: v, likewise */
+  int64_t q_stride_s, q_stride_t, q_stride_h;   /* attend: q [n_seq, n_q, q_heads, head_dim] */
+} mustdrop_page_config_t;
+
+/* Bytes of the pool / of the workspace the calls need with this configuration (0: not a valid one).  The workspace has
+ * 256 bytes where n_q is 0, else also room for mustdrop_page_attend's partial results. */
+size_t mustdrop_page_pool_bytes(const mustdrop_page_config_t *config /* (host) */);
+size_t mustdrop_page_workspace_bytes(const mustdrop_page_config_t *config /* (host) */);
+
+/*
+ * Pages and slots for the tokens sequences gain, and pages back from those that shrink.
+ *   add int32 [n_seq]    tokens sequence s gains; negative: it gives back its last -add[s] tokens (all, if it has fewer)
+ *   len int32 [n_seq]    tokens each sequence holds; len_out (may be len itself) receives the new lengths
+ *   ring int32 [n_pages] a ring of free page ids, ring_state int32 [2] = {head, count}: the free pages are
+ *                        ring[(head + i) mod n_pages], i < count; ring_state_out (may be ring_state) receives the new state
+ *   page_table int32 [n_seq, max_pages]  entry p of row s: the page of tokens p * page ..; entries at and beyond
+ *                        ceil(len/page) mean nothing and are left as they are
+ *   slots int32 [n_seq, rows]  receives the slots of the tokens gained, in order, then -1
+ * New pages are taken from the ring's head, in order of sequence and place; pages given back are appended behind its
+ * count and can be taken by the NEXT call.  A sequence grows completely or not at all: it grows if it needs no new page, or if
+ * the pages it and all sequences before it ask for (refused ones included) are free; otherwise its length stays
+ * and MUSTDROP_ERR_NO_PAGES is recorded.  add[s] > rows, len[s] outside [0, max_pages * page] or growth beyond it:
+ * the sequence stays as it is, MUSTDROP_ERR_BAD_LENGTH is recorded.
+ * Uses n_seq, page, n_pages, max_pages, rows of the configuration.
+ */
+mustdrop_status_t mustdrop_page_tables(const mustdrop_page_config_t *config /* (host) */, const int32_t *add,
+                                       const int32_t *len, const int32_t *ring_state, int32_t *len_out,
+                                       int32_t *ring_state_out, int32_t *ring, int32_t *page_table, int32_t *slots,
+                                       void *workspace, void *cuda_stream);
+
+/*
+ * Quantise rows of K and V into their slots.  k, v bf16 [n_seq, n_heads, rows, head_dim] (strides);
+ * slots int32 [n_seq, rows]: rows with a negative slot are skipped (not read); one at or beyond n_pages * page is skipped and recorded as
+ * MUSTDROP_ERR_BAD_PAGE.  No slot may occur twice.  workspace may be NULL.
+ */
+mustdrop_status_t mustdrop_page_store(const mustdrop_page_config_t *config /* (host) */, const int32_t *slots,
+                                      const void *k, const void *v, void *pool, void *workspace, void *cuda_stream);
+
+/*
+ * The values of stored tokens, rounded to bf16: k_out, v_out bf16 [n_seq, n_heads, rows, head_dim] contiguous;
+ * either may be NULL.  Rows whose slot is negative (or outside the pool: recorded) are left as they are.  workspace
+ * may be NULL.
+ */
+mustdrop_status_t mustdrop_page_load(const mustdrop_page_config_t *config /* (host) */, const int32_t *slots,
+                                     const void *pool, void *k_out, void *v_out, void *workspace, void *cuda_stream);
+
+/*
+ * Attention of the last n_q tokens of every sequence over its pages.
+ *   out[s][t][j] = sum over visible keys x of softmax(scale <q[s][t][j], K_x>) V_x    with K / V head j * n_heads / q_heads
+ * q bf16 [n_seq, n_q, q_heads, head_dim] (strides); page_table int32 [n_seq, max_pages], len int32 [n_seq]: keys
+ * 0 .. len[s]-1 are read through the table (clamped to [0, max_pages * page], recorded as MUSTDROP_ERR_BAD_LENGTH);
+ * out bf16 [n_seq, n_q, q_heads, head_dim] contiguous.  A query token that sees no key gets zeros.  Keys on a page id
+ * outside [0, n_pages) are left out and recorded as MUSTDROP_ERR_BAD_PAGE.  fp32 accumulation, probabilities in
+ * 11 bits; the same call gives the same bits.
+ */
+mustdrop_status_t mustdrop_page_attend(const mustdrop_page_config_t *config /* (host) */, const void *q,
+                                       const void *pool, const int32_t *page_table, const int32_t *len, void *out,
+                                       void *workspace, void *cuda_stream);
 
 /* Kernel launches one mustdrop_filter call enqueues for this plan (-1: invalid plan). */
 int32_t mustdrop_plan_filter_launches(const mustdrop_plan_t *plan);

@@ -25,6 +25,9 @@ MUSTDROP_ERR_CUDA = 5
 MUSTDROP_ERR_TIMEOUT = 6
 MUSTDROP_ERR_BAD_KEY_INDEX = 7
 MUSTDROP_ERR_SCRATCH_LIMIT = 8
+MUSTDROP_ERR_BAD_PAGE = 9
+MUSTDROP_ERR_BAD_LENGTH = 10
+MUSTDROP_ERR_NO_PAGES = 11
 
 MUSTDROP_MODE_BUDGET, MUSTDROP_MODE_THRESHOLD = 0, 1
 MUSTDROP_CRIT_DUAL, MUSTDROP_CRIT_GLOBAL_ONLY, MUSTDROP_CRIT_INDIVIDUAL_ONLY = 0, 1, 2
@@ -35,7 +38,8 @@ EXPORTS = (
     "mustdrop_last_cuda_error", "mustdrop_plan_score_variant", "mustdrop_score_static",
     "mustdrop_score_static_max_rows", "mustdrop_filter", "mustdrop_plan_filter_launches",
     "mustdrop_filter_layer", "mustdrop_cache_compact", "mustdrop_spatial_merge", "mustdrop_key_set",
-    "mustdrop_plan_describe",
+    "mustdrop_plan_describe", "mustdrop_page_pool_bytes", "mustdrop_page_workspace_bytes", "mustdrop_page_tables",
+    "mustdrop_page_store", "mustdrop_page_load", "mustdrop_page_attend",
 )
 
 
@@ -73,6 +77,14 @@ class mustdrop_layer_io_t(ctypes.Structure):
 class mustdrop_cache_config_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "n_layers", "batch", "n_heads", "head_dim", "rows_in", "vis_start", "n_tail", "ids_max", "cap")]
+
+
+class mustdrop_page_config_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_seq", "n_heads", "head_dim", "page", "n_pages", "max_pages", "rows", "q_heads", "n_q", "causal")] + [
+        ("scale", ctypes.c_float), ("flags", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in (
+            "k_stride_s", "k_stride_h", "k_stride_r", "v_stride_s", "v_stride_h", "v_stride_r",
+            "q_stride_s", "q_stride_t", "q_stride_h")]
 
 
 class MustDropError(RuntimeError):
@@ -115,6 +127,11 @@ def lib() -> ctypes.CDLL:
         L.mustdrop_spatial_merge.restype = ctypes.c_int
         L.mustdrop_key_set.argtypes = [i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
         L.mustdrop_key_set.restype = ctypes.c_int
+        L.mustdrop_page_pool_bytes.argtypes = L.mustdrop_page_workspace_bytes.argtypes = [vp]
+        L.mustdrop_page_pool_bytes.restype = L.mustdrop_page_workspace_bytes.restype = ctypes.c_size_t
+        for n, count in (("tables", 11), ("store", 7), ("load", 7), ("attend", 8)):
+            f = getattr(L, "mustdrop_page_" + n)
+            f.argtypes, f.restype = [vp] * count, ctypes.c_int
         L.mustdrop_plan_filter_launches.argtypes = [vp]
         L.mustdrop_plan_filter_launches.restype = ctypes.c_int32
         L.mustdrop_device_status.argtypes = [vp, vp, vp, i32p, i32p]
@@ -280,6 +297,52 @@ def mustdrop_key_set(batch, n_heads, head_dim, n_tokens, key_max, q_cls, k, a_cl
                                   _ptr(mu_out), _ptr(key_idx), _ptr(key_cnt), _stream(stream))
 
 
+class PageConfig:
+    """A mustdrop_page_config_t, built once and handed to every mustdrop_page_* call (keyword arguments: its fields;
+    head_dim defaults to 128, page to 16, causal to 1)."""
+
+    def __init__(self, **sizes):
+        c = mustdrop_page_config_t()
+        c.head_dim, c.page, c.causal = 128, 16, 1
+        names = {n for n, _ in mustdrop_page_config_t._fields_}
+        for n, val in sizes.items():
+            if n not in names:
+                raise TypeError("mustdrop_page_config_t has no field %r" % n)
+            setattr(c, n, float(val) if n == "scale" else int(val))
+        self.c = c
+        self.ref = ctypes.addressof(c)
+
+
+def mustdrop_page_pool_bytes(config: PageConfig) -> int:
+    return lib().mustdrop_page_pool_bytes(config.ref)
+
+
+def mustdrop_page_workspace_bytes(config: PageConfig) -> int:
+    return lib().mustdrop_page_workspace_bytes(config.ref)
+
+
+def mustdrop_page_tables(config: PageConfig, add, len, ring_state, len_out, ring_state_out, ring, page_table, slots,
+                         workspace, stream=None) -> int:
+    return lib().mustdrop_page_tables(config.ref, _ptr(add), _ptr(len), _ptr(ring_state), _ptr(len_out),
+                                      _ptr(ring_state_out), _ptr(ring), _ptr(page_table), _ptr(slots), _ptr(workspace),
+                                      _stream(stream))
+
+
+def mustdrop_page_store(config: PageConfig, slots, k, v, pool, workspace=None, stream=None) -> int:
+    return lib().mustdrop_page_store(config.ref, _ptr(slots), _ptr(k), _ptr(v), _ptr(pool), _ptr(workspace),
+                                     _stream(stream))
+
+
+def mustdrop_page_load(config: PageConfig, slots, pool, k_out, v_out, workspace=None, stream=None) -> int:
+    return lib().mustdrop_page_load(config.ref, _ptr(slots), _ptr(pool), _ptr(k_out), _ptr(v_out), _ptr(workspace),
+                                    _stream(stream))
+
+
+def mustdrop_page_attend(config: PageConfig, q, pool, page_table, len, out, workspace, stream=None) -> int:
+    return lib().mustdrop_page_attend(config.ref, _ptr(q), _ptr(pool), _ptr(page_table), _ptr(len), _ptr(out),
+                                      _ptr(workspace), _stream(stream))
+
+
 def mustdrop_plan_describe(plan) -> str:
     buf = ctypes.create_string_buffer(256)
     L = lib()
@@ -425,3 +488,134 @@ def config_for(w, **overrides) -> Config:
                 key_max=max(w.key_cnt, 0))
     base.update(overrides)
     return Config(**base)
+
+
+class PagedCache:
+    """Convenience owner of a paged 4-bit cache: pool, free ring, page tables, lengths and workspace (torch CUDA tensors).
+
+    n_seq sequences (one per layer and request: layer * batch + request, say) of n_heads K / V heads share n_pages pages.
+    All arithmetic happens in the library calls; this class only allocates and forwards.  Its calls share one workspace:
+    they belong on one stream, or on streams that wait for each other.
+    """
+
+    def __init__(self, n_seq, n_heads, n_pages, max_pages, head_dim=128, page=16, q_heads=None, max_q=1, causal=1, scale=0.0,
+                 device="cuda"):
+        import torch
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.n_seq, self.n_heads, self.head_dim, self.page = n_seq, n_heads, head_dim, page
+        self.q_heads, self.max_q = q_heads or n_heads, max_q
+        self._base = dict(n_heads=n_heads, head_dim=head_dim, page=page, n_pages=n_pages, max_pages=max_pages)
+        self._attend = dict(self._base, q_heads=self.q_heads, causal=causal, scale=scale)
+        self._configs = {}
+        full = PageConfig(n_seq=n_seq, n_q=max_q, **self._attend)
+        pool_bytes, ws_bytes = mustdrop_page_pool_bytes(full), mustdrop_page_workspace_bytes(full)
+        if pool_bytes == 0 or ws_bytes == 0 or max_pages <= 0:
+            raise MustDropError(MUSTDROP_ERR_INVALID_ARG, "PagedCache")
+        i32 = dict(dtype=torch.int32, device=self.device)
+        self.pool = torch.empty(pool_bytes, dtype=torch.uint8, device=self.device)
+        self.workspace = torch.zeros(ws_bytes, dtype=torch.uint8, device=self.device)
+        self.ring = torch.arange(n_pages, **i32)
+        self.ring_state = torch.tensor([0, n_pages], **i32)
+        self.page_table = torch.full((n_seq, max_pages), -1, **i32)
+        self.len = torch.zeros((n_seq,), **i32)
+
+    def _config(self, key, **sizes):
+        c = self._configs.get(key)
+        if c is None:
+            c = self._configs[key] = PageConfig(**sizes)
+        return c
+
+    def _check(self, st, where, tensors):
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise ValueError("%s: a tensor is on %s, the cache on %s" % (where, t.device, self.device))
+        if st is not None and st != MUSTDROP_OK:
+            raise MustDropError(st, where)
+
+    def _on(self):
+        import torch
+        return torch.cuda.device(self.device)
+
+    @staticmethod
+    def _want(t, shape, name):
+        import torch
+        if tuple(t.shape) != tuple(shape) or t.dtype != torch.bfloat16 or t.stride(-1) != 1:
+            raise ValueError("%s: bf16 %s with contiguous rows expected, got %s %s" % (name, tuple(shape), t.dtype, tuple(t.shape)))
+
+    def extend(self, add, rows, slots=None, stream=None):
+        """Every sequence gains add[s] tokens (at most `rows`; negative: gives some back) -> slots int32 [n_seq, rows]."""
+        import torch
+        if add.dtype != torch.int32 or add.numel() != self.n_seq or not add.is_contiguous():
+            raise ValueError("add: contiguous int32 [%d] expected" % self.n_seq)
+        if slots is None:
+            slots = torch.empty((self.n_seq, rows), dtype=torch.int32, device=self.device)
+        elif slots.dtype != torch.int32 or tuple(slots.shape) != (self.n_seq, rows) or not slots.is_contiguous():
+            raise ValueError("slots: contiguous int32 [%d, %d] expected" % (self.n_seq, rows))
+        self._check(None, "extend", (add, slots))
+        c = self._config(("extend", rows), n_seq=self.n_seq, rows=rows, **self._base)
+        with self._on():
+            st = mustdrop_page_tables(c, add, self.len, self.ring_state, self.len, self.ring_state, self.ring, self.page_table,
+                                      slots, self.workspace, stream)
+        self._check(st, "mustdrop_page_tables", ())
+        return slots
+
+    def _rows(self, slots):
+        import torch
+        if slots.dtype != torch.int32 or slots.dim() != 2 or not slots.is_contiguous():
+            raise ValueError("slots: contiguous int32 [sequences, rows] expected")
+        return tuple(slots.shape)
+
+    def store(self, slots, k, v, stream=None):
+        """k, v bf16 [sequences, n_heads, rows, head_dim] (any strides of whole 16 bytes) into `slots` [sequences, rows]."""
+        n, rows = self._rows(slots)
+        for name, t in (("k", k), ("v", v)):
+            self._want(t, (n, self.n_heads, rows, self.head_dim), name)
+        self._check(None, "store", (slots, k, v))
+        ks, vs = k.stride(), v.stride()
+        c = self._config(("store", n, rows, ks, vs), n_seq=n, rows=rows, k_stride_s=ks[0], k_stride_h=ks[1], k_stride_r=ks[2],
+                         v_stride_s=vs[0], v_stride_h=vs[1], v_stride_r=vs[2], **self._base)
+        with self._on():
+            st = mustdrop_page_store(c, slots, k, v, self.pool, self.workspace, stream)
+        self._check(st, "mustdrop_page_store", ())
+
+    def load(self, slots, k_out, v_out, stream=None):
+        """The stored values of `slots` as bf16 rows [sequences, n_heads, rows, head_dim]; rows without a slot stay as they are."""
+        n, rows = self._rows(slots)
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            if t is not None:
+                self._want(t, (n, self.n_heads, rows, self.head_dim), name)
+                if not t.is_contiguous():
+                    raise ValueError("%s: contiguous rows expected" % name)
+        self._check(None, "load", (slots, k_out, v_out))
+        c = self._config(("load", n, rows), n_seq=n, rows=rows, **self._base)
+        with self._on():
+            st = mustdrop_page_load(c, slots, self.pool, k_out, v_out, self.workspace, stream)
+        self._check(st, "mustdrop_page_load", ())
+        return k_out, v_out
+
+    def attend(self, q, first=0, out=None, stream=None):
+        """q bf16 [n, n_q, q_heads, head_dim]: the last n_q tokens of sequences first .. first + n - 1 -> out likewise."""
+        import torch
+        n, n_q = q.shape[0], q.shape[1]
+        self._want(q, (n, n_q, self.q_heads, self.head_dim), "q")
+        if n_q > self.max_q or first < 0 or first + n > self.n_seq:
+            raise ValueError("attend: at most %d query tokens of sequences 0 .. %d" % (self.max_q, self.n_seq - 1))
+        if out is None:
+            out = torch.empty((n, n_q, self.q_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
+        self._want(out, (n, n_q, self.q_heads, self.head_dim), "out")
+        if not out.is_contiguous():
+            raise ValueError("out: contiguous rows expected")
+        self._check(None, "attend", (q, out))
+        qs = q.stride()
+        c = self._config(("attend", n, n_q, qs), n_seq=n, n_q=n_q, q_stride_s=qs[0], q_stride_t=qs[1], q_stride_h=qs[2], **self._attend)
+        with self._on():
+            st = mustdrop_page_attend(c, q, self.pool, self.page_table[first:], self.len[first:], out, self.workspace, stream)
+        self._check(st, "mustdrop_page_attend", ())
+        return out
+
+    def device_status(self):
+        """(code, detail) the calls so far recorded (synchronises)."""
+        import torch
+        return tuple(self.workspace[:8].view(torch.int32).tolist())

@@ -439,6 +439,9 @@ const char* mustdrop_status_string(mustdrop_status_t s) {
     case MUSTDROP_ERR_BAD_KEY_INDEX: return "index outside [0, n_vis) ignored";
     case MUSTDROP_ERR_SCRATCH_LIMIT:
       return "batch * n_heads * n_txt exceeds the built-in scratch of mustdrop_score_static (524288 rows)";
+    case MUSTDROP_ERR_BAD_PAGE: return "page id or slot outside the pool ignored";
+    case MUSTDROP_ERR_BAD_LENGTH: return "sequence length or growth outside its limits refused";
+    case MUSTDROP_ERR_NO_PAGES: return "too few free pages for a sequence";
   }
   return "unknown status";
 }
