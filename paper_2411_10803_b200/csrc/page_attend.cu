@@ -2,20 +2,26 @@
 //
 //   S[x][q] = scale <K_x, q>,  P = exp(S - m),  out[q] = sum_x P V_x / sum_x P,   K = z + s (c - 8) per group of 32 channels
 //
-// With C the codes minus 8 (exact in fp16) and Q the query scaled by a power of two into fp16's range (exact):
-//   <K_x, q> = sum_g s_xg (sum_{d in g} C_xd Q_d)  +  sum_g z_xg (sum_{d in g} Q_d)
-//   out_d    = sum_x (P_x s_xg) C_xd               +  sum_x P_x z_xg
-// so the codes go into the matrix instructions as they are, with 16 tokens (K) or 16 channels (V) as the rows and
-// the query rows - the query tokens and heads that share a K / V head - as the 8 columns: scales meet fp32 accumulators
-// (K) or the probabilities (V), centres are one more instruction each (bf16, the sums over Q in three bf16 terms).
-// P s is rounded once, to fp16: 11 bits; a running power of two keeps it in range whatever the scales are.
+//   <K_x, q> = sum_g s_xg (sum_{d in g} c_xd q_d)  +  sum_g (z_xg - 8 s_xg) (sum_{d in g} q_d)
+//   out_d    = sum_x (P_x s_xg) (c_xd - 8)         +  sum_x P_x z_xg
 //
-// Bound: HBM.  A token and head is 1.25 D bytes where bf16 has 4 D, and unpacking must keep up with ~23 bytes per
-// clock and SM: 9 instructions per 8 codes.  Every warp walks its own range of chunks (16 tokens of one head,
-// 20 D contiguous bytes: one bulk copy each) through its own ring in shared memory, without a barrier between warps.  The chunks of
-// all (sequence, head, row tile) units form one line that is cut into equal parts, one per warp, whatever
-// the lengths are: no host has to know them.  A unit that several warps share is joined by a second kernel from
-// partial results (fp32), in the order of the warps: the same call gives the same bits.
+// so the codes go into the matrix instructions as they are, with 16 tokens (K) or 16 channels (V) as the rows and the query
+// rows - the query tokens and heads that share a K / V head - as the 8 columns.  Scales meet fp32 accumulators (K) or
+// the probabilities (V); the centres are matrix instructions of their own (bf16, the sums over q in three bf16 terms).
+//
+// K in e4m3: a code in the low bits of a byte IS the e4m3 number 2^-9 c, so a word of eight codes costs three instructions.
+// q, scaled by a power of two to a largest member of 128 .. 256, is the sum of two e4m3 numbers but for less than 2^-18 of
+// that member; the products are exact and their sum is fp32 (measured: bit for bit a double sum's nearest fp32 over random
+// operands).  V in fp16, codes minus 8: nine instructions per word, but one rounding of P s to 11 bits, where e4m3 would need
+// three terms.  A running power of two keeps P s in fp16's range whatever the scales are.
+//
+// Bound: HBM.  A token and head is 1.25 D bytes where bf16 has 4 D, and the arithmetic must keep up with ~23 bytes per
+// clock and SM.  Every warp walks its own range of chunks (16 tokens of one head, 20 D contiguous bytes, one bulk copy each), two
+// at a time, through its own ring in shared memory, without a barrier between warps.  The chunks of all (sequence, head, row
+// tile) units form one line that is cut into equal parts, one per warp, whatever the lengths are: no host has
+// to know them.  A unit that several warps share is joined from partial results (fp32): first those of a CTA, behind its last
+// barrier, then those of the CTAs, by the CTA that finishes last.  Both add in the order of the line: the same call gives
+// the same bits.
 #include <algorithm>
 
 #include "page_internal.h"
@@ -23,11 +29,9 @@
 namespace mustdrop {
 namespace {
 
-constexpr int kWarps = 8;             // per CTA
-constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxSeqs = 4096;
-constexpr int kMaxCtas = 320;         // 2 per SM, and some to spare
-constexpr int kMinChunks = 2;         // least chunks per warp where there are enough warps: a shorter range is all set-up
+constexpr int kMaxCtas = 192;         // one per SM, and some to spare
+constexpr size_t kCountBytes = 1024;  // of the workspace: a counter per CTA, zero between calls
 constexpr long long kWaitCycles = 200000000ll;   // ~0.1 s: a bulk copy that takes longer will not come
 
 struct AttendParams {
@@ -35,10 +39,12 @@ struct AttendParams {
   const uint8_t* pool;
   const int32_t *table, *len;
   uint16_t* out;
-  float* part;              // partial results: [2 * warps][rows][D + 2]
+  float* part;              // partial results [CTA][2][part_rows][D + 4]: stabiliser, sum, -, -, D values
+  unsigned* joined;         // [CTA]: parts of the unit that begins in this CTA and ends in a later one
   int32_t* workspace;
   int32_t n_seq, n_heads, group, n_q, rows, tiles;   // rows = n_q * group query rows per unit, in `tiles` row tiles
   int32_t lg, n_pages, max_pages, causal, part_rows;
+  uint32_t group_magic;       // 2^32 / group, rounded up: a row (below 2^14) over the group is the product's high half
   int64_t q_ss, q_st, q_sh;   // bytes
   float scale_log2e;
 };
@@ -64,9 +70,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {   // 
   return true;
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(src), "r"(bytes), "r"(bar)
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
                : "memory");
 }
 __device__ __forceinline__ float ex2(float x) {
@@ -103,112 +107,916 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
 }
 // Nibbles j and j + 4 of a word as fp16 pairs of codes - 8, for j = 0..3.  A nibble under the bits of 1024 reads 1024 + c
 // (bits 0..3) or 1024 + 16 c (bits 4..7); both lose their offset in one exact operation.
-__device__ __forceinline__ void unpack8(uint32_t w, uint32_t (&x)[4]) {
+struct Consts {   // kept in registers: as literals the compiler loads them again for every word
+  uint32_t low, high, magic, sixteenth, minus72;
+};
+__device__ __forceinline__ uint32_t opaque(uint32_t v) {
+  asm volatile("" : "+r"(v));
+  return v;
+}
+__device__ __forceinline__ Consts make_consts() {
+  return {opaque(0x000f000fu), opaque(0x00f000f0u), opaque(0x64006400u), opaque(0x2c002c00u), opaque(0xd480d480u)};   // .., 1/16, -72
+}
+__device__ __forceinline__ void unpack8(const Consts& k, uint32_t w, uint32_t (&x)[4]) {
   const uint32_t w8 = w >> 8;
   uint32_t y[4];
-  asm("lop3.b32 %0, %1, 0x000f000f, 0x64006400, 0xea;" : "=r"(y[0]) : "r"(w));
-  asm("lop3.b32 %0, %1, 0x00f000f0, 0x64006400, 0xea;" : "=r"(y[1]) : "r"(w));
-  asm("lop3.b32 %0, %1, 0x000f000f, 0x64006400, 0xea;" : "=r"(y[2]) : "r"(w8));
-  asm("lop3.b32 %0, %1, 0x00f000f0, 0x64006400, 0xea;" : "=r"(y[3]) : "r"(w8));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[0]) : "r"(w), "r"(k.low), "r"(k.magic));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[1]) : "r"(w), "r"(k.high), "r"(k.magic));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[2]) : "r"(w8), "r"(k.low), "r"(k.magic));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[3]) : "r"(w8), "r"(k.high), "r"(k.magic));
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x[0]) : "r"(y[0]), "r"(0x64086408u));                              // 1032
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[1]) : "r"(y[1]), "r"(0x2c002c00u), "r"(0xd480d480u));         // 1/16, -72
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[1]) : "r"(y[1]), "r"(k.sixteenth), "r"(k.minus72));
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x[2]) : "r"(y[2]), "r"(0x64086408u));
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[3]) : "r"(y[3]), "r"(0x2c002c00u), "r"(0xd480d480u));
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[3]) : "r"(y[3]), "r"(k.sixteenth), "r"(k.minus72));
 }
 
 // The line of chunks: sequence s has heads * tiles units of chunks(s) chunks each.
-__device__ __forceinline__ int32_t clamp_len(const AttendParams& p, int s) {
-  const int64_t most = static_cast<int64_t>(p.max_pages) << p.lg;
-  const int32_t n = p.len[s];
-  return n < 0 ? 0 : n > most ? static_cast<int32_t>(most) : n;
+__device__ __forceinline__ int32_t clamp_len(const AttendParams& p, int32_t n) {
+  const int32_t most = p.max_pages << p.lg;
+  return n < 0 ? 0 : n > most ? most : n;
 }
 __device__ __forceinline__ int32_t chunks_of(int32_t len) { return static_cast<int32_t>((static_cast<uint32_t>(len) + kChunkTokens - 1) / kChunkTokens); }
 
-// Equal parts of the line.  With few chunks fewer warps take part, the same number of every CTA.
+// Equal parts of the line, one per CTA: `more` CTAs have per + 1 chunks, the others per.
 struct Cut {
-  long long total;    // chunks
-  int warps;          // that take part, per_cta of each CTA
-  int per_cta;
-  __device__ __forceinline__ long long begin(int w) const { return total * w / warps; }
-  // the warp that has chunk x
-  __device__ __forceinline__ int owner(long long x) const { return static_cast<int>(((x + 1) * warps - 1) / total); }
+  int ctas, per, more;
+  __device__ __forceinline__ long long begin(int c) const { return static_cast<long long>(c) * per + min(c, more); }
+  // the CTA that has chunk x
+  __device__ __forceinline__ int owner(long long x) const {
+    const long long big = static_cast<long long>(more) * (per + 1);
+    return static_cast<int>(x < big ? divide(x, per + 1) : more + divide(x - big, per));
+  }
+  static __device__ __forceinline__ long long divide(long long a, int b) {   // (a 64-bit division takes some 100 cycles more)
+    return a >> 32 == 0 ? static_cast<uint32_t>(a) / static_cast<uint32_t>(b) : a / b;
+  }
 };
 __device__ __forceinline__ Cut cut_of(long long total, int ctas) {
   Cut c;
-  c.total = total;
-  const long long want = (total + kMinChunks - 1) / kMinChunks;
-  const long long per = (want + ctas - 1) / ctas;
-  c.per_cta = per > kWarps ? kWarps : per < 1 ? 1 : static_cast<int>(per);
-  c.warps = static_cast<int>(total < static_cast<long long>(c.per_cta) * ctas ? total : static_cast<long long>(c.per_cta) * ctas);
+  c.ctas = total < ctas ? static_cast<int>(total) : ctas;
+  c.per = static_cast<int>(Cut::divide(total, c.ctas));
+  c.more = static_cast<int>(total - static_cast<long long>(c.per) * c.ctas);
   return c;
 }
 
-// A place on the line.
-struct Place {
-  int32_t seq, head, tile, chunk, n;   // chunk of n
+// A place in the warp's part of the line: `left` chunks from `chunk` on are of this unit, `rest` chunks come after them.
+struct Cursor {
+  int32_t seq, head, tile, chunk, left, rest;
 };
-__device__ __forceinline__ void step(const AttendParams& p, Place& x, const int32_t* first) {   // first[s]: chunks (per unit) of the sequences before s
-  if (++x.chunk < x.n) return;
+__device__ __forceinline__ void next_unit(const AttendParams& p, Cursor& x, const int32_t* first) {   // first[s]: chunks (per unit) of the sequences before s
   x.chunk = 0;
-  if (++x.tile < p.tiles) return;
-  x.tile = 0;
-  if (++x.head < p.n_heads) return;
-  x.head = 0;
-  do {
-    ++x.seq;
-    x.n = x.seq < p.n_seq ? first[x.seq + 1] - first[x.seq] : 1;
-  } while (x.n == 0);
+  if (++x.tile >= p.tiles) {
+    x.tile = 0;
+    if (++x.head >= p.n_heads) {
+      x.head = 0;
+      do {
+        ++x.seq;
+      } while (x.seq < p.n_seq - 1 && first[x.seq + 1] == first[x.seq]);
+    }
+  }
+  x.left = min(x.rest, first[x.seq + 1] - first[x.seq]);
+  x.rest -= x.left;
 }
 
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  return v;
+}
+// a where c, else b: as an instruction, so that an array of registers is not made an array in memory
+__device__ __forceinline__ float pick(bool c, float a, float b) {
+  float d;
+  asm("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\tselp.f32 %0, %1, %2, p;\n\t}" : "=f"(d) : "f"(a), "f"(b), "r"(static_cast<uint32_t>(c)));
+  return d;
+}
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// Two numbers as e4m3 (low byte: lo), and what an e4m3 pair stands for.
+__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
+  uint16_t h;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(hi), "f"(lo));
+  return h;
+}
+__device__ __forceinline__ void unpack_e4m3(uint32_t b, float& lo, float& hi) {
+  uint32_t w;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(w) : "h"(static_cast<uint16_t>(b)));
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(lo), "=f"(hi) : "r"(w));
+}
+__device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Joins `n` partial results of one query row (in order; at(i) gives the i-th) in one warp: lane's channels 4 lane .. + 3.
+struct RowSum {
+  float m, l;
+  float4 v;
+};
+template <int D, bool OTHERS, typename At>   // OTHERS: parts that other CTAs wrote, past this SM's L1
+__device__ __forceinline__ RowSum join_row(int n, At at, int lane) {
+  RowSum s = {-INFINITY, 0.0f, make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+  const int c = min(lane, D / 4 - 1);
+  constexpr int kBatch = 8;            // loads in flight: parts of other CTAs come from L2
+  for (int base = 0; base < n; base += kBatch) {
+    float2 ml[kBatch];
+    float4 x[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      ml[i] = make_float2(-INFINITY, 0.0f);
+      x[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (base + i < n) {
+        const float* const q = at(base + i);
+        const float2* const a = reinterpret_cast<const float2*>(q);
+        const float4* const b = reinterpret_cast<const float4*>(q + 4) + c;
+        ml[i] = OTHERS ? __ldcg(a) : *a;
+        x[i] = OTHERS ? __ldcg(b) : *b;
+      }
+    }
+    float m = s.m;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) m = fmaxf(m, ml[i].x);
+    const float keep = s.m == -INFINITY ? 0.0f : ex2(s.m - m);
+    s.l *= keep; s.v.x *= keep; s.v.y *= keep; s.v.z *= keep; s.v.w *= keep;
+    s.m = m;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float f = ml[i].x == -INFINITY ? 0.0f : ex2(ml[i].x - m);
+      s.l = fmaf(f, ml[i].y, s.l);
+      s.v.x = fmaf(f, x[i].x, s.v.x); s.v.y = fmaf(f, x[i].y, s.v.y);
+      s.v.z = fmaf(f, x[i].z, s.v.z); s.v.w = fmaf(f, x[i].w, s.v.w);
+    }
+  }
+  return s;
+}
+
+// Query token of a unit's row, and the row's place among the n_q * q_heads rows of its sequence in q and out.
+__device__ __forceinline__ int token_of(const AttendParams& p, int row) { return p.group == 1 ? row : static_cast<int>(__umulhi(row, p.group_magic)); }
+__device__ __forceinline__ int64_t out_row(const AttendParams& p, int row, int head) {
+  const int tq = token_of(p, row);
+  return static_cast<int64_t>(tq * p.n_heads + head) * p.group + (row - tq * p.group);
+}
+__device__ __forceinline__ const uint8_t* q_row(const AttendParams& p, int seq, int head, int row) {
+  const int tq = token_of(p, row);
+  return p.q + seq * p.q_ss + tq * p.q_st + (static_cast<int64_t>(head) * p.group + (row - tq * p.group)) * p.q_sh;
+}
+
+#ifndef NARROW_WARPS
+#define NARROW_WARPS 12
+#define NARROW_STAGES 2
+#endif
+constexpr float kNone = -3.0e38f;   // stabiliser of a column that has seen no key
+
+// What a warp holds of the unit in hand, and its arithmetic, for up to 8 NT query rows: a column each.
 template <int D, int NT>
-struct Shape {
-  static constexpr int kG = D / 32, kTiles = D / 16, kRows = 8 * NT;
-  // chunks in flight per warp: ~100 KB of ring in each of two CTAs per SM
-  static constexpr int kStages = D == 128 ? 5 : 8;
-  static constexpr size_t ring = static_cast<size_t>(kWarps) * kStages * Chunk<D>::kBytes;
+struct Wide {
+  using C = Chunk<D>;
+  static constexpr int kD = D, G = D / 32, kTiles = D / 16, kRows = 8 * NT;
+  // One CTA per SM: 12 warps of up to 168 registers where one column tile needs no more (more warps hide more of a warp's
+  // chain copy - logits - probabilities - out), 8 of 255 for two; ~120 KB of ring.
+  static constexpr int kWarps = NT == 1 ? 12 : 8;
+  static constexpr int kStages = (NT == 1 ? 2 : 3) * (128 / D);
+
+  uint32_t qf[NT][G][4];                   // q as the second operand: two e4m3 terms of two words
+  uint32_t qz[NT][2], qs[NT][2];           // its sums over groups in three bf16 terms, and those times -8
+  float cs[NT][2];                         // log2 units per unit of the scaled product, of columns 2t, 2t + 1
+  float o[NT][kTiles][4], oz[NT][4];    // out (without centres) and the centres' part, rows r, r + 8 and columns 2t, 2t + 1
+  float l[NT][2], m[NT][2];                // sum (of this lane's tokens), stabiliser (kNone: no key seen)
+  float vs_mul = 1.0f;                     // 2^-E: scales of V in units of 2^E
+  uint32_t vs_most = 0;                    // largest bf16 bits of a scale that need no larger E; 0: no E yet
+  int32_t least = 0, len = 0;              // fewest visible keys of any column; the sequence's length
+
+  Consts consts;
+  int lane, r, t;
+
+  __device__ __forceinline__ void init() {
+    lane = threadIdx.x & 31; r = lane >> 2; t = lane & 3;
+    consts = make_consts();
+  }
+
+  __device__ __forceinline__ void fetch(const AttendParams& p, const Cursor& at) {}
+
+  __device__ __forceinline__ void begin(const AttendParams& p, const Cursor& at) {
+    len = clamp_len(p, p.len[at.seq]);
+    least = len;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = at.tile * kRows + nt * 8 + r;
+      uint4 w[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) w[g] = make_uint4(0, 0, 0, 0);
+      if (row < p.rows) {
+        const uint8_t* const src = q_row(p, at.seq, at.head, row) + t * 16;
+#pragma unroll
+        for (int g = 0; g < G; ++g) w[g] = __ldg(reinterpret_cast<const uint4*>(src + g * 64));
+      }
+      float top = 0.0f;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const uint32_t ww[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(bf16_lo(ww[i])), fabsf(bf16_hi(ww[i]))));
+      }
+      top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+      // largest member to [2^7, 2^8)
+      const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);
+      const float up = __uint_as_float(static_cast<uint32_t>(127 + 7 - e) << 23);
+      const float back = __uint_as_float(static_cast<uint32_t>(127 - 7 + e) << 23) * (512.0f * p.scale_log2e);   // (codes are 2^-9 c)
+      float sums[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const uint32_t ww[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(ww[i]) * up; f[2 * i + 1] = bf16_hi(ww[i]) * up; }
+        float s = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+        s += __shfl_xor_sync(~0u, s, 1);
+        s += __shfl_xor_sync(~0u, s, 2);
+        sums[g] = s * (1.0f / 512.0f);
+        // word h: channels h, h + 2, h + 4, h + 6 of the lane's eight (the codes in the low / high halves of a word's bytes)
+#pragma unroll
+        for (int term = 0; term < 2; ++term)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t b01 = pack_e4m3(f[h], f[h + 2]), b23 = pack_e4m3(f[h + 4], f[h + 6]);
+            qf[nt][g][2 * term + h] = b01 | (b23 << 16);
+            float x0, x1, x2, x3;
+            unpack_e4m3(b01, x0, x1);
+            unpack_e4m3(b23, x2, x3);
+            f[h] -= x0; f[h + 2] -= x1; f[h + 4] -= x2; f[h + 6] -= x3;
+          }
+      }
+      // terms of the sums: operand slots 4 term + g (two groups: 2 term + g); lane t holds slots 2t, 2t + 1 and 2t + 8, 2t + 9.
+      // A q that holds no number makes its logits NaN here (the e4m3 conversion would make infinities finite).
+      const bool odd = (G == 4) && (t & 1);
+      float a = odd ? sums[G - 2] : sums[0], b = odd ? sums[G - 1] : sums[1];
+      float whole = 0.0f;
+#pragma unroll
+      for (int g = 0; g < G; ++g) whole += sums[g];
+      uint32_t term[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        term[i] = pack_bf16(a, b);
+        a -= bf16_lo(term[i]);
+        b -= bf16_hi(term[i]);
+      }
+      if (!(fabsf(whole) < INFINITY)) term[0] = term[1] = term[2] = 0x7fff7fffu;
+      if (G == 4) {
+        qz[nt][0] = t < 2 ? term[0] : term[1];
+        qz[nt][1] = t < 2 ? term[2] : 0u;
+      } else {
+        qz[nt][0] = t == 0 ? term[0] : t == 1 ? term[1] : t == 2 ? term[2] : 0u;
+        qz[nt][1] = 0u;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) qs[nt][i] = pack_bf16(-8.0f * bf16_lo(qz[nt][i]), -8.0f * bf16_hi(qz[nt][i]));
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        cs[nt][j] = __shfl_sync(~0u, back, (2 * t + j) * 4);
+        l[nt][j] = 0.0f;
+        m[nt][j] = kNone;
+      }
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) oz[nt][j] = 0.0f;
+    }
+    if (p.causal) least = max(0, len - p.n_q + 1 + token_of(p, at.tile * kRows));
+    vs_mul = 1.0f;
+    vs_most = 0;
+
+  }
+
+  __device__ __forceinline__ void pair(const AttendParams& p, const Cursor& at, uint32_t c0, uint32_t gone) {
+    const int key0 = at.chunk * kChunkTokens;
+    const bool edge = gone != 0 || key0 + 2 * kChunkTokens > least;
+
+    // logits of the tokens 2r (row r) and 2r + 1 (row r + 8) of both chunks
+    float sacc[2][NT][4];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const uint32_t c = c0 + hf * C::kBytes;
+      uint32_t kw[2][G];
+      float ks[2][G];
+      uint32_t kz[2], kss[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t cw = c + C::kK + (r + 8 * h) * (D / 2) + t * (4 * G);
+        const uint32_t cz = c + C::kKsz + (r + 8 * h) * (4 * G);
+        if (G == 4) {
+          const uint4 w = lds128(cw);
+          kw[h][0] = w.x; kw[h][1] = w.y; kw[h][G - 2] = w.z; kw[h][G - 1] = w.w;
+          const uint4 z = lds128(cz);
+          ks[h][0] = bf16_lo(z.x); ks[h][1] = bf16_hi(z.x); ks[h][G - 2] = bf16_lo(z.y); ks[h][G - 1] = bf16_hi(z.y);
+          kss[h] = (t & 1) ? z.y : z.x;
+          kz[h] = (t & 1) ? z.w : z.z;
+        } else {
+          const uint2 w = lds64(cw);
+          kw[h][0] = w.x; kw[h][1] = w.y;
+          const uint2 z = lds64(cz);
+          ks[h][0] = bf16_lo(z.x); ks[h][1] = bf16_hi(z.x);
+          kss[h] = z.x;
+          kz[h] = z.y;
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sacc[hf][nt][j] = 0.0f;
+        mma_bf16(sacc[hf][nt], kz[0], kz[1], kz[0], kz[1], qz[nt][0], qz[nt][1]);
+        mma_bf16(sacc[hf][nt], kss[0], kss[1], kss[0], kss[1], qs[nt][0], qs[nt][1]);
+      }
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const uint32_t a0 = kw[0][g] & 0x0f0f0f0fu, a1 = kw[1][g] & 0x0f0f0f0fu;
+        const uint32_t a2 = (kw[0][g] >> 4) & 0x0f0f0f0fu, a3 = (kw[1][g] >> 4) & 0x0f0f0f0fu;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          mma_e4m3(a, a0, a1, a2, a3, qf[nt][g][0], qf[nt][g][1]);
+          mma_e4m3(a, a0, a1, a2, a3, qf[nt][g][2], qf[nt][g][3]);
+          sacc[hf][nt][0] = fmaf(ks[0][g], a[0], sacc[hf][nt][0]);
+          sacc[hf][nt][1] = fmaf(ks[0][g], a[1], sacc[hf][nt][1]);
+          sacc[hf][nt][2] = fmaf(ks[1][g], a[2], sacc[hf][nt][2]);
+          sacc[hf][nt][3] = fmaf(ks[1][g], a[3], sacc[hf][nt][3]);
+        }
+      }
+    }
+    // V's scales of this lane's tokens (bf16 pairs of groups), its centres as a first operand (rows: groups)
+    uint32_t vsw[2][2][G / 2], vz[2][2];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t c = c0 + hf * C::kBytes;
+        if (G == 4) {
+          const uint2 w = lds64(c + C::kVs + (r + 8 * h) * (2 * G));
+          vsw[hf][h][0] = w.x; vsw[hf][h][G / 2 - 1] = w.y;
+        } else {
+          vsw[hf][h][0] = lds32(c + C::kVs + (r + 8 * h) * (2 * G));
+        }
+        vz[hf][h] = lds32(c + C::kVz + (r & (G - 1)) * 32 + h * 16 + t * 4);
+      }
+    if (edge) {
+      // hidden keys: logits at -inf, and nothing of bytes that were never written
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const int base = key0 + hf * kChunkTokens;
+        const int end = (gone >> hf) & 1u ? base : len;        // keys of the chunk that are there end here
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int key = base + 2 * r + h;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const int col = at.tile * kRows + nt * 8 + 2 * t + j;
+              const int lim = p.causal ? min(end, len - p.n_q + 1 + token_of(p, col)) : end;
+              if (key >= lim) sacc[hf][nt][2 * h + j] = -INFINITY;
+            }
+#pragma unroll
+          for (int g = 0; g < G / 2; ++g)
+            if (key >= end) vsw[hf][h][g] = 0u;
+          const int zk = base + 4 * t + h;                     // tokens of the centres' operand: 4t + h, 4t + 2 + h
+          if (zk >= end) vz[hf][h] &= 0xffff0000u;
+          if (zk + 2 >= end) vz[hf][h] &= 0x0000ffffu;
+        }
+      }
+    }
+    // a logit far above the stabiliser, or a scale far above its unit: move them (rare after the first chunks)
+    float rise[2][NT][4];
+    float high = -INFINITY;
+    uint32_t vs_top = 0;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          rise[hf][nt][j] = fmaf(sacc[hf][nt][j], cs[nt][j & 1], -m[nt][j & 1]);
+          high = fmaxf(high, rise[hf][nt][j]);
+        }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int g = 0; g < G / 2; ++g) vs_top = max_u16x2(vs_top, vsw[hf][h][g]);
+    }
+    vs_top = max(vs_top & 0xffffu, vs_top >> 16);
+    if (__any_sync(~0u, high > 8.0f || vs_top > vs_most)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float top = kNone;
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+            top = fmaxf(top, fmaxf(sacc[hf][nt][j] * cs[nt][j], sacc[hf][nt][j + 2] * cs[nt][j]));
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+          if (top > m[nt][j] + 8.0f) {
+            const float f = ex2(m[nt][j] - top);
+            m[nt][j] = top;
+            l[nt][j] *= f;
+            oz[nt][j] *= f; oz[nt][j + 2] *= f;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) { o[nt][i][j] *= f; o[nt][i][j + 2] *= f; }
+          }
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              rise[hf][nt][j + 2 * h] = fmaf(sacc[hf][nt][j + 2 * h], cs[nt][j], -m[nt][j]);
+        }
+      // A NaN for a scale: NaN in its group's channels (by way of the centres) for the columns that see the key, and the key's
+      // scale is zero from here on: a column that does not see it has P = 0, and 0 x NaN would be one.
+      uint32_t none = 0;               // bit (nt, j, g)
+      vs_top = 0;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const uint32_t half = (g & 1) ? 0xffff0000u : 0x0000ffffu;
+            if ((vsw[hf][h][g >> 1] & half) > (half & 0x7f807f80u)) {
+              vsw[hf][h][g >> 1] &= ~half;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                  if (sacc[hf][nt][2 * h + j] != -INFINITY) none |= 1u << ((nt * 2 + j) * G + g);
+            }
+            const uint32_t v = vsw[hf][h][g >> 1] & half;
+            vs_top = max(vs_top, (g & 1) ? v >> 16 : v);
+          }
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) none |= __shfl_xor_sync(~0u, none, d);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          if (r < G && ((none >> ((nt * 2 + j) * G + r)) & 1u)) oz[nt][j] = __uint_as_float(0x7fffffffu);
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) vs_top = max(vs_top, __shfl_xor_sync(~0u, vs_top, d));
+      if (vs_top > vs_most) {
+        const int e = min(max(static_cast<int>(vs_top >> 7) - 127, -100), 126);
+        const float mul = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        const float f = vs_most == 0 ? 1.0f : mul / vs_mul;
+        vs_mul = mul;
+        vs_most = min(static_cast<uint32_t>(e + 127 + 6) << 7, 0x7f7fu);      // up to 64 units
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[nt][i][j] *= f;
+      }
+    }
+    // probabilities; P and P s, turned into second operands; out
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const uint32_t c = c0 + hf * C::kBytes;
+      uint32_t pv[NT][G][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float pr[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pr[j] = ex2(rise[hf][nt][j]);
+        l[nt][0] += pr[0] + pr[2];
+        l[nt][1] += pr[1] + pr[3];
+        const uint32_t pz0 = transpose8x8(pack_bf16(pr[0], pr[1])), pz1 = transpose8x8(pack_bf16(pr[2], pr[3]));
+        mma_bf16(oz[nt], vz[hf][0], 0u, vz[hf][1], 0u, pz0, pz1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float p0 = pr[2 * h] * vs_mul, p1 = pr[2 * h + 1] * vs_mul;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const float s = (g & 1) ? bf16_hi(vsw[hf][h][g >> 1]) : bf16_lo(vsw[hf][h][g >> 1]);
+            pv[nt][g][h] = transpose8x8(pack_f16(p0 * s, p1 * s));
+          }
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < kTiles / 4; ++a) {
+        const uint4 w = lds128(c + C::kV + (a * 32 + lane) * 16);
+        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t u[4];
+          unpack8(consts, ww[i], u);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            mma_f16(o[nt][4 * a + i], u[0], u[1], u[2], u[3], pv[nt][2 * a + (i >> 1)][0], pv[nt][2 * a + (i >> 1)][1]);
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void end(const AttendParams& p, const Cursor& at, bool whole, float* part) {
+    constexpr int kPart = D + 4;
+    const int64_t out_seq = static_cast<int64_t>(p.rows) * p.n_heads * D;
+    const float unit = 1.0f / vs_mul;        // 2^E
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float sum = l[nt][j];
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        const int in_tile = nt * 8 + 2 * t + j, row = at.tile * kRows + in_tile;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        uint16_t* const dst = p.out + at.seq * out_seq + out_row(p, row, at.head) * D;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const float z = __shfl_sync(~0u, oz[nt][j], g * 4 + t);
+          float v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = fmaf(o[nt][2 * g + (i >> 1)][j + 2 * (i & 1)], unit, z);
+          if (row < p.rows) {
+            const int d0 = 32 * g + 4 * r;
+            if (whole)
+              *reinterpret_cast<uint2*>(dst + d0) = make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
+            else
+              *reinterpret_cast<float4*>(part + in_tile * kPart + 4 + d0) = make_float4(v[0], v[1], v[2], v[3]);
+          }
+        }
+        if (!whole && row < p.rows && r == 0)
+          *reinterpret_cast<float2*>(part + in_tile * kPart) = make_float2(m[nt][j] == kNone ? -INFINITY : m[nt][j], sum);
+      }
+  }
 };
 
-template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) page_attend_kernel(const AttendParams p) {
-  using S = Shape<D, NT>;
+// The same for one or two query rows (one query token, a K / V head to each query head or two): the 8 columns are the 4
+// groups of 32 channels times 2, so a lane deals with one group - column 2t, 2t + 1: group t - and with a quarter of the
+// scales, centres and products that the layout above gives every lane.  The second index of a column is the row, or, with
+// one row, the term of q for the logits.  With 64 channels there are two groups, and columns of the other half hold the
+// second term.  A column's product with another group's channels is zero (logits: its operand is) or not used (out).
+template <int D, int R>
+struct Narrow {
   using C = Chunk<D>;
-  constexpr int G = S::kG, kStages = S::kStages;
-  extern __shared__ __align__(128) uint8_t ring_all[];
+  static constexpr int kD = D, G = D / 32, kTiles = D / 16, kRows = R;
+  static constexpr int kWarps = NARROW_WARPS, kStages = NARROW_STAGES * (128 / D);
+  static constexpr int kTerms = D == 128 && R == 2 ? 2 : 1;   // instructions per group: the terms of q that have no column of their own
+  static constexpr bool kPairSum = D == 128 && R == 1;        // the two columns of a lane are the terms of one row
+
+  uint32_t qf[G][kTerms][2];    // q as the second operand, zero outside the column's group
+  float qs[R], q8[2];           // the sum of q over this lane's group; -8 times it for its columns (zero for second terms)
+  float cs[R], m[R], l[R], oz[R];
+  float o[kTiles][4];
+  float vs_mul;
+  uint32_t vs_most;
+  int32_t least, len;
+  uint4 next_q;
+  int32_t next_len;
+  Consts consts;
+  int lane, r, t;
+
+  __device__ __forceinline__ void init() {
+    lane = threadIdx.x & 31; r = lane >> 2; t = lane & 3;
+    consts = make_consts();
+  }
+
+  // asks for a unit's queries and its length, while the one before is finished: this lane's part of the second operand, column
+  // n = lane / 4, channels 8 t .. + 7 of its group
+  __device__ __forceinline__ void fetch(const AttendParams& p, const Cursor& at) {
+    const int n = lane >> 2, group = (n >> 1) & (G - 1);
+    next_len = p.len[at.seq];
+    next_q = __ldg(reinterpret_cast<const uint4*>(q_row(p, at.seq, at.head, R == 2 ? n & 1 : 0) + group * 64 + t * 16));
+  }
+
+  __device__ __forceinline__ void begin(const AttendParams& p, const Cursor& at) {
+    len = clamp_len(p, next_len);
+    least = p.causal ? max(0, len - p.n_q + 1) : len;
+    const int n = lane >> 2, group = (n >> 1) & (G - 1);
+    const uint32_t ww[4] = {next_q.x, next_q.y, next_q.z, next_q.w};
+    float f[8], top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = bf16_lo(ww[i]);
+      f[2 * i + 1] = bf16_hi(ww[i]);
+      top = fmaxf(top, fmaxf(fabsf(f[2 * i]), fabsf(f[2 * i + 1])));
+    }
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+    const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);   // largest member to [2^7, 2^8)
+    const float up = __uint_as_float(static_cast<uint32_t>(127 + 7 - e) << 23);
+    const float back = __uint_as_float(static_cast<uint32_t>(127 - 7 + e) << 23) * (512.0f * p.scale_log2e);   // (codes are 2^-9 c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] *= up;
+    float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+    sum += __shfl_xor_sync(~0u, sum, 1);
+    sum += __shfl_xor_sync(~0u, sum, 2);
+    uint32_t term[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {   // word h: channels h, h + 2, h + 4, h + 6 (the codes in the low / high halves of a word's bytes)
+        const uint32_t b01 = pack_e4m3(f[h], f[h + 2]), b23 = pack_e4m3(f[h + 4], f[h + 6]);
+        term[k][h] = b01 | (b23 << 16);
+        float x0, x1, x2, x3;
+        unpack_e4m3(b01, x0, x1);
+        unpack_e4m3(b23, x2, x3);
+        f[h] -= x0; f[h + 2] -= x1; f[h + 4] -= x2; f[h + 6] -= x3;
+      }
+    // the term a column holds: with kTerms == 2 both, by turns; else by its place
+    const int second = kPairSum ? n & 1 : n >> 2;
+    const bool unused = D == 64 && R == 1 && (n & 1);
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int k = 0; k < kTerms; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t v = kTerms == 2 ? term[k][h] : second ? term[1][h] : term[0][h];
+          qf[g][k][h] = g == group && !unused ? v : 0u;
+        }
+    // to the lanes that own the columns' products.  A q that holds no number makes its logits NaN here.
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const int from = (2 * t + j) * 4;
+      const float s = __shfl_sync(~0u, sum, from) * (1.0f / 512.0f);
+      cs[j] = __shfl_sync(~0u, back, from);
+      const bool first_term = D == 128 || t < 2;
+      qs[j] = !(fabsf(s) < INFINITY) ? __uint_as_float(0x7fffffffu) : first_term ? s : 0.0f;
+      q8[j] = -8.0f * qs[j];
+      l[j] = 0.0f; m[j] = kNone; oz[j] = 0.0f;
+    }
+    if (R == 1) q8[1] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
+    vs_mul = 1.0f;
+    vs_most = 0;
+  }
+
+  __device__ __forceinline__ void pair(const AttendParams& p, const Cursor& at, uint32_t c0, uint32_t gone) {
+    const int g = t & (G - 1);
+    const int key0 = at.chunk * kChunkTokens;
+    float s[2][2][R];          // logits of tokens 2r, 2r + 1 of both chunks: this lane's group's part, then the whole
+    uint32_t vsb[2][2];        // V scales (bf16 bits) and centres of this lane's tokens and group
+    float vz[2][2];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const uint32_t c = c0 + hf * C::kBytes;
+      float a[4] = {q8[0], q8[1], q8[0], q8[1]};
+      uint32_t kw[2][G];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t cw = c + C::kK + (r + 8 * h) * (D / 2) + t * (4 * G);
+        if (G == 4) {
+          const uint4 w = lds128(cw);
+          kw[h][0] = w.x; kw[h][1] = w.y; kw[h][G - 2] = w.z; kw[h][G - 1] = w.w;
+        } else {
+          const uint2 w = lds64(cw);
+          kw[h][0] = w.x; kw[h][1] = w.y;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const uint32_t a0 = kw[0][i] & 0x0f0f0f0fu, a1 = kw[1][i] & 0x0f0f0f0fu;
+        const uint32_t a2 = (kw[0][i] >> 4) & 0x0f0f0f0fu, a3 = (kw[1][i] >> 4) & 0x0f0f0f0fu;
+#pragma unroll
+        for (int k = 0; k < kTerms; ++k) mma_e4m3(a, a0, a1, a2, a3, qf[i][k][0], qf[i][k][1]);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t cz = c + C::kKsz + (r + 8 * h) * (4 * G) + 2 * g;
+        const float ks = bf16_lo(lds16(cz)), kz = bf16_lo(lds16(cz + 2 * G));
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+          const float x = kPairSum ? a[2 * h] + a[2 * h + 1] : a[2 * h + j];
+          s[hf][h][j] = fmaf(ks, x, kz * qs[j]);
+        }
+        vsb[hf][h] = lds16(c + C::kVs + (r + 8 * h) * (2 * G) + 2 * g);
+        vz[hf][h] = bf16_lo(lds16(c + C::kVz + g * 32 + (r + 8 * h) * 2));
+      }
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+          s[hf][h][j] += __shfl_xor_sync(~0u, s[hf][h][j], 1);
+          s[hf][h][j] += __shfl_xor_sync(~0u, s[hf][h][j], 2);
+        }
+    if (gone != 0 || key0 + 2 * kChunkTokens > least) {
+      // hidden keys: logits at -inf, and nothing of bytes that were never written
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const int base = key0 + hf * kChunkTokens;
+        const int end = (gone >> hf) & 1u ? base : len;        // keys of the chunk that are there end here
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int key = base + 2 * r + h;
+#pragma unroll
+          for (int j = 0; j < R; ++j)
+            if (key >= (p.causal ? min(end, len - p.n_q + 1 + token_of(p, j)) : end)) s[hf][h][j] = -INFINITY;
+          if (key >= end) { vsb[hf][h] = 0u; vz[hf][h] = 0.0f; }
+        }
+      }
+    }
+    // a logit far above the stabiliser, or a scale far above its unit: move them (rare after the first chunks)
+    float high = -INFINITY;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < R; ++j) high = fmaxf(high, fmaf(s[hf][h][j], cs[j], -m[j]));
+    uint32_t vs_top = max(max(vsb[0][0], vsb[0][1]), max(vsb[1][0], vsb[1][1]));
+    if (__any_sync(~0u, high > 8.0f || vs_top > vs_most)) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        float top = fmaxf(fmaxf(s[0][0][j], s[0][1][j]) * cs[j], fmaxf(s[1][0][j], s[1][1][j]) * cs[j]);
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        if (top > m[j] + 8.0f) {
+          const float f = ex2(m[j] - top);
+          m[j] = top;
+          l[j] *= f;
+          oz[j] *= f;
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) { o[i][j] *= f; o[i][j + 2] *= f; }
+        }
+      }
+      // A NaN for a scale: NaN in its group's channels (by way of the centres) for the rows that see the key, and the key's
+      // scale is zero from here on: a row that does not see it has P = 0, and 0 x NaN would be one.
+      vs_top = 0;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (vsb[hf][h] > 0x7f80u) {
+            vsb[hf][h] = 0;
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+              if (s[hf][h][j] != -INFINITY) oz[j] = __uint_as_float(0x7fffffffu);
+          }
+          vs_top = max(vs_top, vsb[hf][h]);
+        }
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) vs_top = max(vs_top, __shfl_xor_sync(~0u, vs_top, d));
+      if (vs_top > vs_most) {
+        const int e = min(max(static_cast<int>(vs_top >> 7) - 127, -100), 126);
+        const float mul = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        const float f = vs_most == 0 ? 1.0f : mul / vs_mul;
+        vs_mul = mul;
+        vs_most = min(static_cast<uint32_t>(e + 127 + 6) << 7, 0x7f7fu);      // up to 64 units
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[i][j] *= f;
+      }
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const uint32_t c = c0 + hf * C::kBytes;
+      uint32_t pv[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float vs = __uint_as_float(vsb[hf][h] << 16) * vs_mul;
+        float u[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+          const float pr = ex2(fmaf(s[hf][h][j], cs[j], -m[j]));
+          l[j] += pr;
+          oz[j] = fmaf(pr, vz[hf][h], oz[j]);
+          u[j] = pr * vs;
+        }
+        pv[h] = transpose8x8(pack_f16(u[0], u[1]));
+      }
+#pragma unroll
+      for (int a = 0; a < kTiles / 4; ++a) {
+        const uint4 w = lds128(c + C::kV + (a * 32 + lane) * 16);
+        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t u[4];
+          unpack8(consts, ww[i], u);
+          mma_f16(o[4 * a + i], u[0], u[1], u[2], u[3], pv[0], pv[1]);
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void end(const AttendParams& p, const Cursor& at, bool whole, float* part) {
+    constexpr int kPart = D + 4;
+    const float unit = 1.0f / vs_mul;        // 2^E
+    const int64_t out_seq = static_cast<int64_t>(p.rows) * p.n_heads * D;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      float sum = l[j], z = oz[j];
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) {
+        sum += __shfl_xor_sync(~0u, sum, d);
+        z += __shfl_xor_sync(~0u, z, d);
+      }
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = o[i >> 1][j + 2 * (i & 1)];
+#pragma unroll
+        for (int g = 1; g < G; ++g) v[i] = pick(t == g, o[2 * g + (i >> 1)][j + 2 * (i & 1)], v[i]);
+        v[i] = fmaf(v[i], unit, z);
+      }
+      const int d0 = 32 * t + 4 * r;
+      if (whole) {
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        uint16_t* const dst = p.out + at.seq * out_seq + out_row(p, j, at.head) * D;
+        if (t < G) *reinterpret_cast<uint2*>(dst + d0) = make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
+      } else {
+        if (t < G) *reinterpret_cast<float4*>(part + j * kPart + 4 + d0) = make_float4(v[0], v[1], v[2], v[3]);
+        if (lane == 0) *reinterpret_cast<float2*>(part + j * kPart) = make_float2(m[j] == kNone ? -INFINITY : m[j], sum);
+      }
+    }
+  }
+};
+
+template <typename Body>
+struct Shared {   // dynamic shared memory of the kernel, from its start
+  static constexpr int kPart = Body::kD + 4;    // floats of a partial result's row: stabiliser, sum, -, -, values
+  static constexpr int kPair = 2 * Chunk<Body::kD>::kBytes;
+  static constexpr int kWarpRing = Body::kStages * kPair;
+  static constexpr int kHeadPart = Body::kRows * kPart * 4;             // bytes of a warp's first partial result
+  static constexpr int kHeads = Body::kWarps * kWarpRing;
+  static constexpr int kFirst = kHeads + Body::kWarps * kHeadPart;      // int32 [n_seq + 1]
+  static_assert(Body::kRows * kPart * 4 <= kWarpRing, "a warp's last partial result lies in its ring");
+};
+
+template <typename Body>
+__global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const AttendParams p) {
+  using Sh = Shared<Body>;
+  constexpr int D = Body::kD, kStages = Body::kStages, kWarps = Body::kWarps, kThreads = 32 * kWarps, kRows = Body::kRows;
+  constexpr int kPart = Sh::kPart, kPair = Sh::kPair, kBytes = Chunk<D>::kBytes;
+  extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars[kWarps][kStages];
-  __shared__ int32_t warp_sum[kWarps];
-  int32_t* const first = reinterpret_cast<int32_t*>(ring_all + S::ring);   // [n_seq + 1]
+  __shared__ int32_t warp_sum[2][kWarps];
+  __shared__ int32_t part_unit[kWarps][2];      // unit of a warp's first / last partial result, -1: none
+  __shared__ int last_s[2];
+  __shared__ __align__(16) float join_s[kWarps][kPart];
+  int32_t* const first = reinterpret_cast<int32_t*>(smem + Sh::kFirst);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int r = lane >> 2, t = lane & 3;
   const uint32_t bar0 = smem_u32(&bars[warp][0]);
-  const uint8_t* const ring = ring_all + static_cast<size_t>(warp) * kStages * C::kBytes;
-  const uint32_t ring0 = smem_u32(ring);
+  const uint32_t ring = smem_u32(smem) + warp * Sh::kWarpRing;
   if (lane == 0) {
     for (int i = 0; i < kStages; ++i) mbar_init(bar0 + 8 * i);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async;" ::: "memory");
   }
+  if (lane < 2) part_unit[warp][lane] = -1;
   pdl_launch_dependents();
   pdl_wait();
 
   // chunks (per unit) of the sequences before each one: 32 bits, as the host refuses more; the line has 64
-  int32_t carry = 0;
+  int32_t carry = 0, longest = 0;
   for (int base = 0; base < p.n_seq; base += kThreads) {
     const int s = base + threadIdx.x;
-    int32_t v = s < p.n_seq ? chunks_of(clamp_len(p, s)) : 0;
-    if (s < p.n_seq && blockIdx.x == 0 && clamp_len(p, s) != p.len[s]) record_status(p.workspace, MUSTDROP_ERR_BAD_LENGTH, s);
+    int32_t v = 0;
+    if (s < p.n_seq) {
+      const int32_t given = p.len[s], n = clamp_len(p, given);
+      v = chunks_of(n);
+      if (blockIdx.x == 0 && n != given) record_status(p.workspace, MUSTDROP_ERR_BAD_LENGTH, s);
+    }
+    const int32_t top = __reduce_max_sync(~0u, v);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int32_t u = __shfl_up_sync(~0u, v, d);
       if (lane >= d) v += u;
     }
-    __syncthreads();
-    if (lane == 31) warp_sum[warp] = v;
+    if (base > 0) __syncthreads();
+    if (lane == 31) { warp_sum[0][warp] = v; warp_sum[1][warp] = top; }
     __syncthreads();
     int32_t all = 0;
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const int32_t u = warp_sum[w];
+      const int32_t u = warp_sum[0][w];
       if (w < warp) v += u;
       all += u;
+      longest = max(longest, warp_sum[1][w]);
     }
     if (s < p.n_seq) first[s + 1] = carry + v;
     carry += all;
@@ -216,484 +1024,274 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) page_attend_kernel(
   if (threadIdx.x == 0) first[0] = 0;
   __syncthreads();
   const int units_per_seq = p.n_heads * p.tiles;
-  const Cut cut = cut_of(static_cast<long long>(carry) * units_per_seq, gridDim.x);
-  if (cut.total == 0 || warp >= cut.per_cta) return;
-  const int lw = blockIdx.x * cut.per_cta + warp;
-  if (lw >= cut.warps) return;
-  const long long begin = cut.begin(lw), end = cut.begin(lw + 1);
+  const int64_t out_seq = static_cast<int64_t>(p.rows) * p.n_heads * D;      // elements of out per sequence
 
-  Place at;       // where the warp computes
+  // ---------------------------------------------------------------- sequences without keys: zeros
+  for (int s = blockIdx.x; s < p.n_seq; s += gridDim.x)
+    if (first[s + 1] == first[s])
+      for (int64_t i = threadIdx.x; i < out_seq / 8; i += kThreads)
+        *reinterpret_cast<uint4*>(p.out + s * out_seq + i * 8) = make_uint4(0, 0, 0, 0);
+  if (carry == 0) return;
+
+  // This CTA's part of the line.  Where every unit can have a CTA of its own and no warp then gets more than four chunks, it has:
+  // nothing is joined across CTAs (one request, 32 heads, 640 keys: 8.6 us against 12.3).
+  const long long total = static_cast<long long>(carry) * units_per_seq;
+  const Cut cut = cut_of(total, gridDim.x);
+  const bool own_unit = static_cast<long long>(p.n_seq) * units_per_seq <= gridDim.x && longest <= 4 * kWarps;
+  auto unit_begin = [&](int unit, int* n) {
+    const int seq = unit / units_per_seq;
+    *n = first[seq + 1] - first[seq];
+    return static_cast<long long>(first[seq]) * units_per_seq + static_cast<long long>(unit - seq * units_per_seq) * *n;
+  };
+  long long line0, line1;
+  if (own_unit) {
+    if (static_cast<int>(blockIdx.x) >= p.n_seq * units_per_seq) return;
+    int n;
+    line0 = unit_begin(blockIdx.x, &n);
+    line1 = line0 + n;
+  } else {
+    if (static_cast<int>(blockIdx.x) >= cut.ctas) return;
+    line0 = cut.begin(blockIdx.x);
+    line1 = cut.begin(blockIdx.x + 1);
+  }
+  if (line0 == line1) return;
+  // Its warps share it by pairs of chunks.
+  const int pairs = static_cast<int>((line1 - line0 + 1) / 2), n_warps = min(pairs, kWarps);
+  auto warp_begin = [&](int w) { return min(line0 + 2 * static_cast<long long>(static_cast<uint32_t>(pairs) / n_warps * w + min(w, static_cast<int>(static_cast<uint32_t>(pairs) % n_warps))), line1); };
+
+  if (warp < n_warps) {
+    Cursor at;       // where the warp computes
+    {
+      const long long begin = warp_begin(warp);
+      int lo = 0, hi = p.n_seq - 1;          // the sequence with first[s] * units <= begin < first[s + 1] * units
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (static_cast<long long>(first[mid + 1]) * units_per_seq <= begin) lo = mid + 1; else hi = mid;
+      }
+      const long long rem = begin - static_cast<long long>(first[lo]) * units_per_seq;
+      const int n = first[lo + 1] - first[lo];
+      const int unit = static_cast<int>(Cut::divide(rem, n));
+      at.seq = lo;
+      at.chunk = static_cast<int>(rem - static_cast<long long>(unit) * n);
+      at.head = p.tiles == 1 ? unit : unit / p.tiles;
+      at.tile = unit - at.head * p.tiles;
+      at.rest = static_cast<int>(warp_begin(warp + 1) - begin);
+      at.left = min(at.rest, n - at.chunk);
+      at.rest -= at.left;
+    }
+    const int per_page = p.lg - 4;           // log2 of the chunks per page
+    const uint32_t in_page = (1u << per_page) - 1;
+    Body body;
+    body.init();
+    body.fetch(p, at);
+
+    // Copies run kStages pairs of chunks ahead of the computation, page ids one pair further.  Lanes 0 and 1 have a chunk each.
+    Cursor ahead = at;
+    struct Ask { int32_t id, off, n; };      // page id and place in the page of this lane's chunk, chunks of the pair (0: none is left)
+    uint32_t bad = ~0u;                      // two bits per stage: chunks that are on no page of the pool, or none at all
+    auto ask = [&]() {
+      Ask a = {-1, 0, 0};
+      if (ahead.left == 0) {
+        if (ahead.rest == 0) return a;
+        next_unit(p, ahead, first);
+      }
+      a.n = min(ahead.left, 2);
+      const int c = ahead.chunk + (lane & 1);
+      if ((lane & 1) < a.n) a.id = __ldg(p.table + (ahead.seq * p.max_pages + (c >> per_page)));
+      a.off = (ahead.head << per_page) + (c & in_page);
+      ahead.chunk += a.n;
+      ahead.left -= a.n;
+      return a;
+    };
+    auto issue = [&](int stage, const Ask& a) {
+      const bool fine = static_cast<uint32_t>(a.id) < static_cast<uint32_t>(p.n_pages);
+      const uint32_t have = __ballot_sync(~0u, fine) & 3u;
+      bad = (bad & ~(3u << (2 * stage))) | ((have ^ 3u) << (2 * stage));
+      const uint32_t bar = bar0 + 8 * stage;
+      if (lane == 0 && have != 0)
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(have == 3u ? kPair : kBytes) : "memory");
+      __syncwarp();
+      if (lane < a.n) {
+        if (fine)
+          bulk_load(ring + stage * kPair + lane * kBytes,
+                    p.pool + (((static_cast<int64_t>(a.id) * p.n_heads) << per_page) + a.off) * kBytes, kBytes, bar);
+        else
+          record_status(p.workspace, MUSTDROP_ERR_BAD_PAGE, a.id);
+      }
+    };
+    Ask next;
+    {
+      Ask begin[kStages];
+#pragma unroll
+      for (int i = 0; i < kStages; ++i) begin[i] = ask();
+      next = ask();
+#pragma unroll
+      for (int i = 0; i < kStages; ++i)
+        if (begin[i].n > 0) issue(i, begin[i]);
+    }
+
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    while (true) {
+      const bool from_start = at.chunk == 0;
+      body.begin(p, at);
+      while (at.left > 0) {
+        const uint32_t gone = (bad >> (2 * stage)) & 3u;
+        if (gone != 3u) {
+          if (!mbar_wait(bar0 + 8 * stage, (phase >> stage) & 1u)) { ok = false; break; }
+          phase ^= 1u << stage;
+          body.pair(p, at, ring + stage * kPair, gone);
+        }
+        const int n = min(at.left, 2);
+        at.chunk += n;
+        at.left -= n;
+        // the stage is free: the pair kStages further on
+        __syncwarp();
+        if (next.n > 0) {
+          issue(stage, next);
+          next = ask();
+        } else {
+          bad |= 3u << (2 * stage);
+        }
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+      }
+      if (!ok) break;
+      // the unit, or the warp's part, ends: results out
+      const Cursor was = at;
+      if (at.rest > 0) {
+        next_unit(p, at, first);
+        body.fetch(p, at);
+      }
+      const bool whole = from_start && was.chunk == first[was.seq + 1] - first[was.seq];
+      if (!whole && lane == 0) part_unit[warp][from_start] = (was.seq * p.n_heads + was.head) * p.tiles + was.tile;
+      // A unit that began before the warp is its first; one that it leaves unfinished is its last: then its ring is idle.
+      body.end(p, was, whole, reinterpret_cast<float*>(smem + (from_start ? warp * Sh::kWarpRing : Sh::kHeads + warp * Sh::kHeadPart)));
+      if (at.left == 0) break;
+    }
+    if (!ok) {
+      // gave up: leave only when the copies in flight have landed (bounded)
+      if (lane == 0) record_status(p.workspace, MUSTDROP_ERR_TIMEOUT, blockIdx.x);
+      for (int i = 0; i < kStages; ++i)
+        if (((bad >> (2 * i)) & 3u) != 3u) (void)mbar_wait(bar0 + 8 * i, (phase >> i) & 1u);
+    }
+  }
+
+  // ---------------------------------------------------------------- joining
+  // A unit whose parts are all in this CTA gets its output; of the others - at most the one the CTA begins in and the one it
+  // ends in - the CTA leaves one part for the CTA that comes last.  Parts of a unit: the last one of the warp it begins in (none,
+  // if it began before the CTA), then the first ones of the warps that follow.
+  __syncthreads();
+  auto write_out = [&](int unit, int in_tile, const RowSum& s) {
+    const int seq = unit / units_per_seq, u = unit - seq * units_per_seq;
+    const int head = p.tiles == 1 ? u : u / p.tiles, row = (u - head * p.tiles) * kRows + in_tile;
+    const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;
+    if (lane < D / 4)
+      *reinterpret_cast<uint2*>(p.out + seq * out_seq + out_row(p, row, head) * D + 4 * lane) =
+          make_uint2(pack_bf16(s.v.x * inv, s.v.y * inv), pack_bf16(s.v.z * inv, s.v.w * inv));
+  };
+  auto rows_of = [&](int unit) { return p.tiles == 1 ? p.rows : min(kRows, p.rows - (unit % p.tiles) * kRows); };
+  int open[2] = {-1, -1};           // units of the parts this CTA leaves: that began before it, that begins in it
   {
-    int lo = 0, hi = p.n_seq - 1;          // the sequence with first[s] * units <= begin < first[s + 1] * units
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (static_cast<long long>(first[mid + 1]) * units_per_seq <= begin) lo = mid + 1; else hi = mid;
-    }
-    const long long rem = begin - static_cast<long long>(first[lo]) * units_per_seq;
-    at.seq = lo;
-    at.n = first[lo + 1] - first[lo];
-    const int unit = static_cast<int>(rem / at.n);
-    at.chunk = static_cast<int>(rem % at.n);
-    at.head = unit / p.tiles;
-    at.tile = unit % p.tiles;
-  }
-  const int per_page = p.lg - 4;           // log2 of the chunks per page
-  const uint32_t in_page = (1u << per_page) - 1;
-
-  // Copies run kStages chunks ahead of the computation, page ids one chunk further.
-  Place ahead = at;
-  long long asked = begin;                 // chunks whose page id has been loaded
-  int32_t next_id = 0, next_off = 0;
-  uint32_t bad = 0;                        // stages whose chunk lies on no page of the pool
-  auto ask = [&]() {
-    if (asked < end) {
-      next_id = __ldg(p.table + static_cast<int64_t>(ahead.seq) * p.max_pages + (ahead.chunk >> per_page));
-      next_off = (ahead.head << per_page) + (ahead.chunk & in_page);
-      step(p, ahead, first);
-    }
-    ++asked;
-  };
-  auto issue = [&](int stage) {
-    const bool fine = static_cast<uint32_t>(next_id) < static_cast<uint32_t>(p.n_pages);
-    bad = (bad & ~(1u << stage)) | (fine ? 0u : 1u << stage);
-    if (lane == 0) {
-      if (fine)
-        bulk_load(ring0 + stage * C::kBytes, p.pool + (((static_cast<int64_t>(next_id) * p.n_heads) << per_page) + next_off) * C::kBytes,
-                  C::kBytes, bar0 + 8 * stage);
-      else
-        record_status(p.workspace, MUSTDROP_ERR_BAD_PAGE, next_id);
-    }
-  };
-  ask();
-  long long issued = begin;
-  for (int i = 0; i < kStages && issued < end; ++i, ++issued) {
-    issue(i);
-    ask();
-  }
-
-  uint32_t qf[NT][G][4];                   // Q as the second operand: [g][2 m + {0, 1}]
-  uint32_t qz[NT][2];                      // its sums over groups, three bf16 terms
-  float cs[NT][2];                         // log2 units per unit of the scaled product, of columns 2t, 2t + 1
-  float o[NT][S::kTiles][4], oz[NT][4];    // out (without centres) and the centres' part, rows r, r + 8 and columns 2t, 2t + 1
-  float l[NT][2], m[NT][2], thr[NT][2];    // sum (of this lane's tokens), stabiliser, rise of a logit that moves it
-  float vs_mul = 1.0f;                     // 2^-E: scales of V in units of 2^E
-  bool vs_set = false;
-  int32_t lim[NT][2];                      // visible keys of columns 2t, 2t + 1
-  int32_t least = 0, len = 0;              // fewest of any column; the sequence's length
-  int32_t seg_first = at.chunk;            // first chunk of the segment in hand
-  bool fresh = true;
-
-  int stage = 0;
-  uint32_t phase = 0;
-  bool ok = true;
-  for (long long x = begin; x < end; ++x) {
-    if (fresh) {
-      // ------------------------------------------------------------ a unit begins: its queries
-      fresh = false;
-      seg_first = at.chunk;
-      len = clamp_len(p, at.seq);
-      least = len;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int row = at.tile * S::kRows + nt * 8 + r;
-        uint4 w[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g) w[g] = make_uint4(0, 0, 0, 0);
-        if (row < p.rows) {
-          const uint8_t* src = p.q + at.seq * p.q_ss + (row / p.group) * p.q_st +
-                               (static_cast<int64_t>(at.head) * p.group + row % p.group) * p.q_sh + t * 16;
-#pragma unroll
-          for (int g = 0; g < G; ++g) w[g] = __ldg(reinterpret_cast<const uint4*>(src + g * 64));
-        }
-        float top = 0.0f;
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const uint32_t ww[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(bf16_lo(ww[i])), fabsf(bf16_hi(ww[i]))));
-        }
-        top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-        // largest member to [2^14, 2^15)
-        const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);
-        const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
-        const float back = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * p.scale_log2e;
-        float sums[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const uint32_t ww[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
-          float f[8];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(ww[i]) * up; f[2 * i + 1] = bf16_hi(ww[i]) * up; }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) qf[nt][g][i] = pack_f16(f[i], f[i + 4]);
-          float s = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-          s += __shfl_xor_sync(~0u, s, 1);
-          s += __shfl_xor_sync(~0u, s, 2);
-          sums[g] = s;
-        }
-        // terms: k slots 4 term + g (two groups: 2 term + g); lane t holds slots 2t, 2t + 1 and 2t + 8, 2t + 9
-        const bool odd = (G == 4) && (t & 1);
-        float a = odd ? sums[G - 2] : sums[0], b = odd ? sums[G - 1] : sums[1];
-        uint32_t term[3];
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-          term[i] = pack_bf16(a, b);
-          a -= bf16_lo(term[i]);
-          b -= bf16_hi(term[i]);
-        }
-        if (G == 4) {
-          qz[nt][0] = t < 2 ? term[0] : term[1];
-          qz[nt][1] = t < 2 ? term[2] : 0u;
+    const int heads = lane < kWarps ? part_unit[lane][0] : -1, tails = lane < kWarps ? part_unit[lane][1] : -1;
+    uint32_t begins = __ballot_sync(~0u, tails >= 0) << 1 | (__shfl_sync(~0u, heads, 0) >= 0 ? 1u : 0u);   // bit w + 1: a unit begins in warp w
+    int task = 0;
+    while (begins != 0) {
+      const int w = __ffs(begins) - 2;          // -1: it began before the CTA
+      begins &= begins - 1;
+      const int unit = w < 0 ? __shfl_sync(~0u, heads, 0) : __shfl_sync(~0u, tails, w);
+      const uint32_t in = __ballot_sync(~0u, heads == unit);
+      const int lead = w >= 0 ? 1 : 0, n = lead + __popc(in), w1 = in != 0 ? __ffs(in) - 1 : 0;
+      int chunks;
+      const bool here = unit_begin(unit, &chunks) + chunks <= line1 && w >= 0;
+      if (!here) open[lead] = unit;
+      const int rows = rows_of(unit);
+      for (int row = (warp + kWarps - task % kWarps) % kWarps; row < rows; row += kWarps) {
+        const RowSum s = join_row<D, false>(n, [&](int k) {
+          const int at = k < lead ? w * Sh::kWarpRing : Sh::kHeads + (w1 + k - lead) * Sh::kHeadPart;
+          return reinterpret_cast<const float*>(smem + at) + row * kPart;
+        }, lane);
+        if (here) {
+          write_out(unit, row, s);
         } else {
-          qz[nt][0] = t == 0 ? term[0] : t == 1 ? term[1] : t == 2 ? term[2] : 0u;
-          qz[nt][1] = 0u;
+          float* const to = p.part + static_cast<size_t>((2 * blockIdx.x + lead) * p.part_rows + row) * kPart;
+          if (lane < D / 4) *reinterpret_cast<float4*>(to + 4 + 4 * lane) = s.v;
+          if (lane == 0) *reinterpret_cast<float2*>(to) = make_float2(s.m, s.l);
         }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          cs[nt][j] = __shfl_sync(~0u, back, (2 * t + j) * 4);
-          const int col = at.tile * S::kRows + nt * 8 + 2 * t + j;
-          lim[nt][j] = p.causal ? min(len, max(0, len - p.n_q + 1 + col / p.group)) : len;
-          l[nt][j] = 0.0f; m[nt][j] = 0.0f; thr[nt][j] = -INFINITY;
-          if (col < p.rows) least = min(least, lim[nt][j]);
-        }
-#pragma unroll
-        for (int i = 0; i < S::kTiles; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) oz[nt][j] = 0.0f;
       }
-      least = min(least, __shfl_xor_sync(~0u, least, 1));
-      least = min(least, __shfl_xor_sync(~0u, least, 2));
-      vs_mul = 1.0f;
-      vs_set = false;
+      task += rows;
     }
-
-    // -------------------------------------------------------------- one chunk
-    const bool there = ((bad >> stage) & 1u) == 0;
-    if (there && !mbar_wait(bar0 + 8 * stage, (phase >> stage) & 1u)) { ok = false; break; }
-    if (there) {
-      phase ^= 1u << stage;
-      const uint8_t* const c = ring + stage * C::kBytes;
-      const int key0 = at.chunk * kChunkTokens + 2 * r;    // tokens of this lane's rows: key0 (row r), key0 + 1 (row r + 8)
-      const bool edge = at.chunk * kChunkTokens + kChunkTokens > least;
-
-      // logits
-      float sacc[NT][4];
-      {
-        uint32_t kw[2][G];
-        float ks[2][G];
-        uint32_t kz[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint8_t* const cw = c + C::kK + (r + 8 * h) * (D / 2) + t * (4 * G);
-          const uint8_t* const cz = c + C::kKsz + (r + 8 * h) * (4 * G);
-          if (G == 4) {
-            const uint4 w = *reinterpret_cast<const uint4*>(cw);
-            kw[h][0] = w.x; kw[h][1] = w.y; kw[h][G - 2] = w.z; kw[h][G - 1] = w.w;
-            const uint4 z = *reinterpret_cast<const uint4*>(cz);
-            ks[h][0] = bf16_lo(z.x); ks[h][1] = bf16_hi(z.x); ks[h][G - 2] = bf16_lo(z.y); ks[h][G - 1] = bf16_hi(z.y);
-            kz[h] = (t & 1) ? z.w : z.z;
-          } else {
-            const uint2 w = *reinterpret_cast<const uint2*>(cw);
-            kw[h][0] = w.x; kw[h][1] = w.y;
-            const uint2 z = *reinterpret_cast<const uint2*>(cz);
-            ks[h][0] = bf16_lo(z.x); ks[h][1] = bf16_hi(z.x);
-            kz[h] = z.y;
-          }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sacc[nt][j] = 0.0f;
-          mma_bf16(sacc[nt], kz[0], kz[1], kz[0], kz[1], qz[nt][0], qz[nt][1]);
-        }
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          uint32_t u0[4], u1[4];
-          unpack8(kw[0][g], u0);
-          unpack8(kw[1][g], u1);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            mma_f16(a, u0[0], u1[0], u0[1], u1[1], qf[nt][g][0], qf[nt][g][1]);
-            mma_f16(a, u0[2], u1[2], u0[3], u1[3], qf[nt][g][2], qf[nt][g][3]);
-            sacc[nt][0] = fmaf(ks[0][g], a[0], sacc[nt][0]);
-            sacc[nt][1] = fmaf(ks[0][g], a[1], sacc[nt][1]);
-            sacc[nt][2] = fmaf(ks[1][g], a[2], sacc[nt][2]);
-            sacc[nt][3] = fmaf(ks[1][g], a[3], sacc[nt][3]);
-          }
-        }
-      }
-      // V's scales of this lane's tokens, its centres as a first operand (rows: groups)
-      float vs[2][G];
-      uint32_t vz[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint8_t* const cv = c + C::kVs + (r + 8 * h) * (2 * G);
-        if (G == 4) {
-          const uint2 w = *reinterpret_cast<const uint2*>(cv);
-          vs[h][0] = bf16_lo(w.x); vs[h][1] = bf16_hi(w.x); vs[h][G - 2] = bf16_lo(w.y); vs[h][G - 1] = bf16_hi(w.y);
-        } else {
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(cv);
-          vs[h][0] = bf16_lo(w); vs[h][1] = bf16_hi(w);
-        }
-        vz[h] = *reinterpret_cast<const uint32_t*>(c + C::kVz + (r & (G - 1)) * 32 + h * 16 + t * 4);
-      }
-      if (edge) {
-        // hidden keys: logits at -inf, and nothing of bytes that were never written
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (key0 + (j >> 1) >= lim[nt][j & 1]) sacc[nt][j] = -INFINITY;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-          for (int g = 0; g < G; ++g)
-            if (key0 + h >= len) vs[h][g] = 0.0f;
-          const int kz0 = at.chunk * kChunkTokens + 4 * t + h;   // tokens of the centres' operand: 4t + h, 4t + 2 + h
-          if (kz0 >= len) vz[h] &= 0xffff0000u;
-          if (kz0 + 2 >= len) vz[h] &= 0x0000ffffu;
-        }
-      }
-      // a logit far above the stabiliser, or a scale far above its unit: move them (rare after the first chunks)
-      float rise[NT][4];
-      bool move = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          rise[nt][j] = fmaf(sacc[nt][j], cs[nt][j & 1], -m[nt][j & 1]);
-          move = move || rise[nt][j] > thr[nt][j & 1];
-        }
-      float vs_top = 0.0f;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int g = 0; g < G; ++g) vs_top = fmaxf(vs_top, vs[h][g]);
-      move = move || vs_top * vs_mul > 64.0f || !vs_set;
-      if (__any_sync(~0u, move)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            float top = fmaxf(rise[nt][j], rise[nt][j + 2]);
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-            if (top > thr[nt][j]) {
-              const float to = m[nt][j] + top;
-              const float f = thr[nt][j] == -INFINITY ? 0.0f : ex2(m[nt][j] - to);   // (nothing summed yet: whatever the factor)
-              thr[nt][j] = 8.0f;
-              m[nt][j] = to;
-              l[nt][j] *= f;
-              oz[nt][j] *= f; oz[nt][j + 2] *= f;
-#pragma unroll
-              for (int i = 0; i < S::kTiles; ++i) { o[nt][i][j] *= f; o[nt][i][j + 2] *= f; }
-#pragma unroll
-              for (int i = 0; i < 2; ++i) rise[nt][j + 2 * i] = fmaf(sacc[nt][j + 2 * i], cs[nt][j], -m[nt][j]);
-            }
-          }
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) vs_top = fmaxf(vs_top, __shfl_xor_sync(~0u, vs_top, d));
-        if (!vs_set || vs_top * vs_mul > 64.0f) {
-          const int e = min(max(static_cast<int>((__float_as_uint(vs_top) >> 23) & 0xff) - 127, -100), 126);
-          const float mul = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-          const float f = vs_set ? mul / vs_mul : 1.0f;
-          vs_set = true;
-          vs_mul = mul;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < S::kTiles; ++i)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) o[nt][i][j] *= f;
-        }
-      }
-      // probabilities; P and P s, turned into second operands
-      uint32_t pz[NT][2], pv[NT][G][2];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float pr[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) pr[j] = ex2(rise[nt][j]);
-        l[nt][0] += pr[0] + pr[2];
-        l[nt][1] += pr[1] + pr[3];
-        pz[nt][0] = transpose8x8(pack_bf16(pr[0], pr[1]));
-        pz[nt][1] = transpose8x8(pack_bf16(pr[2], pr[3]));
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float p0 = pr[2 * h] * vs_mul, p1 = pr[2 * h + 1] * vs_mul;
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            float a = p0 * vs[h][g], b = p1 * vs[h][g];
-            if (edge) {                        // a hidden key's scale may be a NaN
-              if (key0 + h >= lim[nt][0]) a = 0.0f;
-              if (key0 + h >= lim[nt][1]) b = 0.0f;
-            }
-            pv[nt][g][h] = transpose8x8(pack_f16(a, b));
-          }
-        }
-      }
-      // out
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_bf16(oz[nt], vz[0], 0u, vz[1], 0u, pz[nt][0], pz[nt][1]);
-#pragma unroll
-      for (int a = 0; a < S::kTiles / 4; ++a) {
-        const uint4 w = *reinterpret_cast<const uint4*>(c + C::kV + (a * 32 + lane) * 16);
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t u[4];
-          unpack8(ww[i], u);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            mma_f16(o[nt][4 * a + i], u[0], u[1], u[2], u[3], pv[nt][2 * a + (i >> 1)][0], pv[nt][2 * a + (i >> 1)][1]);
-        }
-      }
-    }
-    // the stage is free: the chunk kStages further on
-    __syncwarp();
-    if (issued < end) {
-      issue(stage);
-      ask();
-      ++issued;
-    }
-    stage = stage + 1 == kStages ? 0 : stage + 1;
-
-    // -------------------------------------------------------------- the unit, or the range, ends: results out
-    const bool unit_ends = at.chunk + 1 == at.n;
-    if (unit_ends || x + 1 == end) {
-      const bool whole = unit_ends && seg_first == 0;
-      const float unit = 1.0f / vs_mul;        // 2^E
-      float* const part = p.part + static_cast<size_t>(2 * lw + (seg_first == 0 ? 1 : 0)) * p.part_rows * (D + 2);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float sum = l[nt][j];
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
-          const int in_tile = nt * 8 + 2 * t + j, row = at.tile * S::kRows + in_tile;
-          const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            const float z = __shfl_sync(~0u, oz[nt][j], g * 4 + t);
-            float v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = fmaf(o[nt][2 * g + (i >> 1)][j + 2 * (i & 1)], unit, z);
-            if (row < p.rows) {
-              const int d0 = 32 * g + 4 * r;
-              if (whole) {
-                const int tq = row / p.group, j_head = at.head * p.group + row % p.group;
-                uint16_t* dst = p.out + ((static_cast<int64_t>(at.seq) * p.n_q + tq) * (static_cast<int64_t>(p.n_heads) * p.group) + j_head) * D + d0;
-                *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
-              } else {
-                float* dst = part + in_tile * (D + 2) + 2 + d0;
-                *reinterpret_cast<float2*>(dst) = make_float2(v[0], v[1]);
-                *reinterpret_cast<float2*>(dst + 2) = make_float2(v[2], v[3]);
-              }
-            }
-          }
-          if (!whole && row < p.rows && r == 0)
-            *reinterpret_cast<float2*>(part + in_tile * (D + 2)) = make_float2(thr[nt][j] == -INFINITY ? -INFINITY : m[nt][j], sum);
-        }
-      fresh = true;
-    }
-    step(p, at, first);
   }
-  if (!ok) {
-    // gave up: leave only when the copies in flight have landed (bounded)
-    if (lane == 0) record_status(p.workspace, MUSTDROP_ERR_TIMEOUT, lw);
-    for (int i = 0; i < kStages; ++i)
-      if (((bad >> i) & 1u) == 0 && i < end - begin) (void)mbar_wait(bar0 + 8 * i, (phase >> i) & 1u);
+  if (open[0] < 0 && open[1] < 0) return;
+  __syncthreads();
+  // the counter of a unit is its first CTA's
+  if (threadIdx.x < 2) {
+    const int unit = open[threadIdx.x];
+    int last = 0;
+    if (unit >= 0) {
+      int n;
+      const long long b = unit_begin(unit, &n);
+      const int c0 = cut.owner(b), c1 = cut.owner(b + n - 1);
+      __threadfence();
+      if (atomicInc(p.joined + c0, c1 - c0) == static_cast<unsigned>(c1 - c0)) last = 1;
+      __threadfence();
+    }
+    last_s[threadIdx.x] = last;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (!last_s[k]) continue;
+    const int unit = open[k];
+    int n;
+    const long long b = unit_begin(unit, &n);
+    const int c0 = cut.owner(b), parts = cut.owner(b + n - 1) - c0 + 1, rows = rows_of(unit);
+    const int share = max(1, kWarps / rows);        // warps of a row, each joining a run of the parts
+    const int run = (parts + share - 1) / share;
+    for (int base = 0; base < rows; base += kWarps / share) {
+      const int row = base + warp / share, mine = warp % share;
+      const bool busy = warp < (kWarps / share) * share && row < rows;
+      const int from = min(mine * run, parts), to = min(from + run, parts);
+      if (busy) {
+        const RowSum s = join_row<D, true>(to - from, [&](int i) {
+          const int c = c0 + from + i;
+          return p.part + static_cast<size_t>((2 * c + (c == c0 ? 1 : 0)) * p.part_rows + row) * kPart;
+        }, lane);
+        if (share == 1) {
+          write_out(unit, row, s);
+        } else {
+          if (lane < D / 4) *reinterpret_cast<float4*>(&join_s[warp][4 + 4 * lane]) = s.v;
+          if (lane == 0) *reinterpret_cast<float2*>(&join_s[warp][0]) = make_float2(s.m, s.l);
+        }
+      }
+      if (share > 1) {
+        __syncthreads();
+        if (busy && mine == 0) write_out(unit, row, join_row<D, false>(share, [&](int i) { return &join_s[warp + i][0]; }, lane));
+        __syncthreads();
+      }
+    }
   }
 }
 
-// Joins the units that several warps share, and writes zeros for sequences without keys.  One CTA per (unit, row).
-constexpr int kJoinThreads = 512;
+// Query rows of a tile for `rows` of a unit.
+int tile_rows(int64_t rows) { return rows <= 2 ? static_cast<int>(rows) : rows <= 8 ? 8 : 16; }
+
+template <typename Body>
+cudaError_t launch_attend(const AttendParams& p, int sms, cudaStream_t stream) {
+  const size_t smem = Shared<Body>::kFirst + (static_cast<size_t>(p.n_seq) + 1) * sizeof(int32_t);
+  const cudaError_t e = ensure_kernel_attributes(reinterpret_cast<const void*>(page_attend_kernel<Body>), false);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(page_attend_kernel<Body>, dim3(static_cast<unsigned>(std::min(kMaxCtas, sms))), dim3(32 * Body::kWarps), smem, stream, p);
+}
 
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) page_join_kernel(const AttendParams p, int ctas, int kRows) {
-  constexpr int kParts = kJoinThreads / D;   // threads of a channel, each joining every kParts-th partial result
-  __shared__ long long sums[2][kJoinThreads / 32];
-  __shared__ float acc_s[kJoinThreads], l_s[kJoinThreads];
-  pdl_launch_dependents();
-  const int unit = blockIdx.x, row_in = blockIdx.y;
-  const int units_per_seq = p.n_heads * p.tiles;
-  const int seq = unit / units_per_seq, u = unit % units_per_seq, head = u / p.tiles, tile = u % p.tiles;
-  const int row = tile * kRows + row_in;
-  if (row >= p.rows) { pdl_wait(); return; }
-  pdl_wait();
-  long long before = 0, total = 0;
-  for (int s = threadIdx.x; s < p.n_seq; s += kJoinThreads) {
-    const int n = chunks_of(clamp_len(p, s));
-    total += n;
-    if (s < seq) before += n;
+cudaError_t launch_attend(const AttendParams& p, int tile, int sms, cudaStream_t stream) {
+  switch (tile) {
+    case 1: return launch_attend<Narrow<D, 1>>(p, sms, stream);
+    case 2: return launch_attend<Narrow<D, 2>>(p, sms, stream);
+    case 8: return launch_attend<Wide<D, 1>>(p, sms, stream);
+    default: return launch_attend<Wide<D, 2>>(p, sms, stream);
   }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    before += __shfl_xor_sync(~0u, before, d);
-    total += __shfl_xor_sync(~0u, total, d);
-  }
-  if ((threadIdx.x & 31) == 0) { sums[0][threadIdx.x >> 5] = before; sums[1][threadIdx.x >> 5] = total; }
-  __syncthreads();
-  before = total = 0;
-#pragma unroll
-  for (int w = 0; w < kJoinThreads / 32; ++w) { before += sums[0][w]; total += sums[1][w]; }
-  const int n = chunks_of(clamp_len(p, seq));
-  const int d = threadIdx.x % D, part0 = threadIdx.x / D;
-  const int tq = row / p.group, j_head = head * p.group + row % p.group;
-  uint16_t* const dst = p.out + ((static_cast<int64_t>(seq) * p.n_q + tq) * (static_cast<int64_t>(p.n_heads) * p.group) + j_head) * D + d;
-  if (n == 0) {
-    if (part0 == 0) *dst = 0;
-    return;
-  }
-  const Cut cut = cut_of(total * units_per_seq, ctas);
-  const long long c0 = before * units_per_seq + static_cast<long long>(u) * n;
-  const int w0 = cut.owner(c0), w1 = cut.owner(c0 + n - 1);
-  if (w0 == w1) return;   // one warp had it all
-  // slot 1 of the warp in whose range the unit begins, slot 0 of the others
-  auto at = [&](int w) { return p.part + (static_cast<size_t>(2 * w + (w == w0 ? 1 : 0)) * p.part_rows + row_in) * (D + 2); };
-  float m = -INFINITY;
-  for (int w = w0 + threadIdx.x; w <= w1; w += kJoinThreads) m = fmaxf(m, at(w)[0]);
-#pragma unroll
-  for (int i = 16; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, i));
-  if ((threadIdx.x & 31) == 0) acc_s[threadIdx.x >> 5] = m;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kJoinThreads / 32; ++i) m = fmaxf(m, acc_s[i]);
-  __syncthreads();
-  float acc = 0.0f, l = 0.0f;
-  for (int w = w0 + part0; w <= w1; w += kParts) {
-    const float* const q = at(w);
-    const float f = q[0] == -INFINITY ? 0.0f : ex2(q[0] - m);
-    l = fmaf(f, q[1], l);
-    acc = fmaf(f, q[2 + d], acc);
-  }
-  acc_s[threadIdx.x] = acc;
-  l_s[threadIdx.x] = l;
-  __syncthreads();
-  if (part0 != 0) return;
-#pragma unroll
-  for (int i = 1; i < kParts; ++i) { acc += acc_s[i * D + d]; l += l_s[i * D + d]; }
-  const float v = l == 0.0f ? 0.0f : acc / l;
-  *dst = static_cast<uint16_t>(pack_bf16(v, 0.0f) & 0xffffu);
-}
-
-int tiles_of(int rows) { return rows <= 8 ? 1 : 2; }   // column tiles of 8 query rows
-
-template <int D, int NT>
-cudaError_t launch_attend(const AttendParams& p, int ctas, cudaStream_t stream) {
-  using S = Shape<D, NT>;
-  const size_t smem = S::ring + (static_cast<size_t>(p.n_seq) + 1) * sizeof(int32_t);
-  cudaError_t e = ensure_kernel_attributes(reinterpret_cast<const void*>(page_attend_kernel<D, NT>), false);
-  if (e != cudaSuccess) return e;
-  e = launch_pdl(page_attend_kernel<D, NT>, dim3(static_cast<unsigned>(ctas)), dim3(kThreads), smem, stream, p);
-  if (e != cudaSuccess) return e;
-  const dim3 grid(static_cast<unsigned>(p.n_seq * p.n_heads * p.tiles), static_cast<unsigned>(std::min(p.rows, S::kRows)));
-  return launch_pdl(page_join_kernel<D>, grid, dim3(kJoinThreads), 0, stream, p, ctas, S::kRows);
 }
 
 }  // namespace
@@ -701,9 +1299,9 @@ cudaError_t launch_attend(const AttendParams& p, int ctas, cudaStream_t stream) 
 size_t page_attend_partial_bytes(const mustdrop_page_config_t* c) {
   if (c->n_heads <= 0 || c->q_heads <= 0 || c->q_heads % c->n_heads != 0 || c->n_q > 128) return 0;
   const int64_t rows = static_cast<int64_t>(c->q_heads / c->n_heads) * c->n_q;
-  const size_t part_rows = static_cast<size_t>(std::min<int64_t>(rows, 8 * tiles_of(static_cast<int>(std::min<int64_t>(rows, 64)))));
-  const size_t bytes = static_cast<size_t>(kMaxCtas) * kWarps * 2 * part_rows * (c->head_dim + 2) * sizeof(float);
-  return (bytes + 255) / 256 * 256;
+  const size_t part_rows = static_cast<size_t>(std::min<int64_t>(rows, tile_rows(rows)));
+  const size_t bytes = static_cast<size_t>(kMaxCtas) * 2 * part_rows * (c->head_dim + 4) * sizeof(float);
+  return kCountBytes + (bytes + 255) / 256 * 256;
 }
 
 }  // namespace mustdrop
@@ -732,15 +1330,17 @@ extern "C" mustdrop_status_t mustdrop_page_attend(const mustdrop_page_config_t* 
   AttendParams p = {};
   p.q = static_cast<const uint8_t*>(q); p.pool = static_cast<const uint8_t*>(pool);
   p.table = page_table; p.len = len; p.out = static_cast<uint16_t*>(out);
-  p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWsStatusBytes);
+  p.joined = reinterpret_cast<unsigned*>(static_cast<uint8_t*>(workspace) + kWsStatusBytes);
+  p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWsStatusBytes + kCountBytes);
   p.workspace = static_cast<int32_t*>(workspace);
   p.n_seq = c->n_seq; p.n_heads = c->n_heads; p.group = c->q_heads / c->n_heads; p.n_q = c->n_q;
   p.rows = static_cast<int32_t>(rows);
-  const int nt = tiles_of(p.rows);
-  p.tiles = (p.rows + 8 * nt - 1) / (8 * nt);
-  p.part_rows = std::min(p.rows, 8 * nt);
+  p.group_magic = static_cast<uint32_t>((1ull << 32) / static_cast<uint32_t>(p.group)) + 1u;
+  const int tile = tile_rows(rows);
+  p.tiles = (p.rows + tile - 1) / tile;
+  p.part_rows = std::min(p.rows, tile);
   if (static_cast<int64_t>(p.n_seq) * p.n_heads * p.tiles > INT32_MAX ||
-      static_cast<int64_t>(p.n_heads) * p.tiles > (1ll << 50) / most)     // (places on the line times warps: 63 bits)
+      static_cast<int64_t>(p.n_heads) * p.tiles > (1ll << 36) / most)     // (a CTA's part of the line: 31 bits on 64 CTAs)
     return MUSTDROP_ERR_UNSUPPORTED;
   p.lg = page_log2(c->page); p.n_pages = c->n_pages; p.max_pages = c->max_pages; p.causal = c->causal;
   p.q_sh = 2 * (c->q_stride_h != 0 ? c->q_stride_h : c->head_dim);
@@ -752,12 +1352,8 @@ extern "C" mustdrop_status_t mustdrop_page_attend(const mustdrop_page_config_t* 
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e == cudaSuccess) {
-    const int ctas = std::min(kMaxCtas, sms * (nt == 1 ? 2 : 1));
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (c->head_dim == 128)
-      e = nt == 1 ? launch_attend<128, 1>(p, ctas, stream) : launch_attend<128, 2>(p, ctas, stream);
-    else
-      e = nt == 1 ? launch_attend<64, 1>(p, ctas, stream) : launch_attend<64, 2>(p, ctas, stream);
+    e = c->head_dim == 128 ? launch_attend<128>(p, tile, sms, stream) : launch_attend<64>(p, tile, sms, stream);
   }
   if (e == cudaSuccess) return MUSTDROP_OK;
   set_last_cuda_error(e);
