@@ -2,18 +2,17 @@
 //
 //   S[x][q] = scale <K_x, q>,  P = exp(S - m),  out[q] = sum_x P V_x / sum_x P,   K = z + s (c - 8) per group of 32 channels
 //
-//   <K_x, q> = sum_g s_xg (sum_{d in g} c_xd q_d)  +  sum_g (z_xg - 8 s_xg) (sum_{d in g} q_d)
-//   out_d    = sum_x (P_x s_xg) (c_xd - 8)         +  sum_x P_x z_xg
+//   <K_x, q> = sum_g s_xg (sum_{d in g} C_xd q_d)  +  sum_g z_xg (sum_{d in g} q_d)         C = c - 8
+//   out_d    = sum_x (P_x s_xg) C_xd               +  sum_x P_x z_xg
 //
 // so the codes go into the matrix instructions as they are, with 16 tokens (K) or 16 channels (V) as the rows and the query
 // rows - the query tokens and heads that share a K / V head - as the 8 columns.  Scales meet fp32 accumulators (K) or
-// the probabilities (V); the centres are matrix instructions of their own (bf16, the sums over q in three bf16 terms).
-//
-// K in e4m3: a code in the low bits of a byte IS the e4m3 number 2^-9 c, so a word of eight codes costs three instructions.
-// q, scaled by a power of two to a largest member of 128 .. 256, is the sum of two e4m3 numbers but for less than 2^-18 of
-// that member; the products are exact and their sum is fp32 (measured: bit for bit a double sum's nearest fp32 over random
-// operands).  V in fp16, codes minus 8: nine instructions per word, but one rounding of P s to 11 bits, where e4m3 would need
-// three terms.  A running power of two keeps P s in fp16's range whatever the scales are.
+// the probabilities (V).  Codes are fp16 operands (exact); q is scaled by a power of two into fp16's range (exact but for
+// members below 2^-29 of the largest); P s is rounded once, to 11 bits, with a running power of two that keeps it in fp16's
+// range whatever the scales are.  A word of eight codes costs nine instructions (five of bits, four to take the offset off); K saves
+// two of them: half of its codes go in as 64 + c, and 72 times the sum of q over their channels is taken off again, which costs
+// four bits of fp32's 24 there; over the many tokens of V's sums it would cost more.  (e4m3 operands, in which a code is a code's
+// own bits, were slower: this GPU runs that instruction as two of fp16 behind conversions.)
 //
 // Bound: HBM.  A token and head is 1.25 D bytes where bf16 has 4 D, and the arithmetic must keep up with ~23 bytes per
 // clock and SM.  Every warp walks its own range of chunks (16 tokens of one head, 20 D contiguous bytes, one bulk copy each), two
@@ -105,7 +104,7 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Nibbles j and j + 4 of a word as fp16 pairs of codes - 8, for j = 0..3.  A nibble under the bits of 1024 reads 1024 + c
+// Nibbles j and j + 4 of a word as fp16 pairs of codes - 8, for j = 0..3 (K: of 1024 + 16 c for j = 1, 3).  A nibble under the bits of 1024 reads 1024 + c
 // (bits 0..3) or 1024 + 16 c (bits 4..7); both lose their offset in one exact operation.
 struct Consts {   // kept in registers: as literals the compiler loads them again for every word
   uint32_t low, high, magic, sixteenth, minus72;
@@ -117,6 +116,7 @@ __device__ __forceinline__ uint32_t opaque(uint32_t v) {
 __device__ __forceinline__ Consts make_consts() {
   return {opaque(0x000f000fu), opaque(0x00f000f0u), opaque(0x64006400u), opaque(0x2c002c00u), opaque(0xd480d480u)};   // .., 1/16, -72
 }
+template <bool CENTRED>
 __device__ __forceinline__ void unpack8(const Consts& k, uint32_t w, uint32_t (&x)[4]) {
   const uint32_t w8 = w >> 8;
   uint32_t y[4];
@@ -125,9 +125,14 @@ __device__ __forceinline__ void unpack8(const Consts& k, uint32_t w, uint32_t (&
   asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[2]) : "r"(w8), "r"(k.low), "r"(k.magic));
   asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[3]) : "r"(w8), "r"(k.high), "r"(k.magic));
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x[0]) : "r"(y[0]), "r"(0x64086408u));                              // 1032
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[1]) : "r"(y[1]), "r"(k.sixteenth), "r"(k.minus72));
+  if (CENTRED) {
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[1]) : "r"(y[1]), "r"(k.sixteenth), "r"(k.minus72));
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[3]) : "r"(y[3]), "r"(k.sixteenth), "r"(k.minus72));
+  } else {
+    x[1] = y[1];
+    x[3] = y[3];
+  }
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x[2]) : "r"(y[2]), "r"(0x64086408u));
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[3]) : "r"(y[3]), "r"(k.sixteenth), "r"(k.minus72));
 }
 
 // The line of chunks: sequence s has heads * tiles units of chunks(s) chunks each.
@@ -146,7 +151,7 @@ struct Cut {
     const long long big = static_cast<long long>(more) * (per + 1);
     return static_cast<int>(x < big ? divide(x, per + 1) : more + divide(x - big, per));
   }
-  static __device__ __forceinline__ long long divide(long long a, int b) {   // (a 64-bit division takes some 100 cycles more)
+  static __device__ __noinline__ long long divide(long long a, int b) {   // (a 64-bit division takes some 100 cycles more; one copy, as all that runs once is fetched first)
     return a >> 32 == 0 ? static_cast<uint32_t>(a) / static_cast<uint32_t>(b) : a / b;
   }
 };
@@ -208,23 +213,6 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
-// Two numbers as e4m3 (low byte: lo), and what an e4m3 pair stands for.
-__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
-  uint16_t h;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(hi), "f"(lo));
-  return h;
-}
-__device__ __forceinline__ void unpack_e4m3(uint32_t b, float& lo, float& hi) {
-  uint32_t w;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(w) : "h"(static_cast<uint16_t>(b)));
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(lo), "=f"(hi) : "r"(w));
-}
-__device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
 // Joins `n` partial results of one query row (in order; at(i) gives the i-th) in one warp: lane's channels 4 lane .. + 3.
 struct RowSum {
   float m, l;
@@ -234,7 +222,7 @@ template <int D, bool OTHERS, typename At>   // OTHERS: parts that other CTAs wr
 __device__ __forceinline__ RowSum join_row(int n, At at, int lane) {
   RowSum s = {-INFINITY, 0.0f, make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
   const int c = min(lane, D / 4 - 1);
-  constexpr int kBatch = 8;            // loads in flight: parts of other CTAs come from L2
+  constexpr int kBatch = OTHERS ? 8 : 2;   // loads in flight: parts of other CTAs come from L2
   for (int base = 0; base < n; base += kBatch) {
     float2 ml[kBatch];
     float4 x[kBatch];
@@ -294,8 +282,8 @@ struct Wide {
   static constexpr int kWarps = NT == 1 ? 12 : 8;
   static constexpr int kStages = (NT == 1 ? 2 : 3) * (128 / D);
 
-  uint32_t qf[NT][G][4];                   // q as the second operand: two e4m3 terms of two words
-  uint32_t qz[NT][2], qs[NT][2];           // its sums over groups in three bf16 terms, and those times -8
+  uint32_t qf[NT][G][4];                   // q as the second operand: [g][2 m + {0, 1}], odd channels over 16
+  uint32_t qz[NT][2], qs[NT][2];           // its sums over groups, and over their odd channels times -72, in three bf16 terms
   float cs[NT][2];                         // log2 units per unit of the scaled product, of columns 2t, 2t + 1
   float o[NT][kTiles][4], oz[NT][4];    // out (without centres) and the centres' part, rows r, r + 8 and columns 2t, 2t + 1
   float l[NT][2], m[NT][2];                // sum (of this lane's tokens), stabiliser (kNone: no key seen)
@@ -336,58 +324,50 @@ struct Wide {
       }
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-      // largest member to [2^7, 2^8)
+      // largest member to [2^14, 2^15)
       const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);
-      const float up = __uint_as_float(static_cast<uint32_t>(127 + 7 - e) << 23);
-      const float back = __uint_as_float(static_cast<uint32_t>(127 - 7 + e) << 23) * (512.0f * p.scale_log2e);   // (codes are 2^-9 c)
-      float sums[G];
+      const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
+      const float back = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * p.scale_log2e;
+      float sums[G], odds[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const uint32_t ww[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
         float f[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(ww[i]) * up; f[2 * i + 1] = bf16_hi(ww[i]) * up; }
-        float s = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qf[nt][g][i] = (i & 1) ? pack_f16(f[i] * 0.0625f, f[i + 4] * 0.0625f) : pack_f16(f[i], f[i + 4]);
+        float odd = (f[1] + f[3]) + (f[5] + f[7]), s = odd + ((f[0] + f[2]) + (f[4] + f[6]));
         s += __shfl_xor_sync(~0u, s, 1);
         s += __shfl_xor_sync(~0u, s, 2);
-        sums[g] = s * (1.0f / 512.0f);
-        // word h: channels h, h + 2, h + 4, h + 6 of the lane's eight (the codes in the low / high halves of a word's bytes)
-#pragma unroll
-        for (int term = 0; term < 2; ++term)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t b01 = pack_e4m3(f[h], f[h + 2]), b23 = pack_e4m3(f[h + 4], f[h + 6]);
-            qf[nt][g][2 * term + h] = b01 | (b23 << 16);
-            float x0, x1, x2, x3;
-            unpack_e4m3(b01, x0, x1);
-            unpack_e4m3(b23, x2, x3);
-            f[h] -= x0; f[h + 2] -= x1; f[h + 4] -= x2; f[h + 6] -= x3;
-          }
+        odd += __shfl_xor_sync(~0u, odd, 1);
+        odd += __shfl_xor_sync(~0u, odd, 2);
+        sums[g] = s;
+        odds[g] = -72.0f * odd;
       }
       // terms of the sums: operand slots 4 term + g (two groups: 2 term + g); lane t holds slots 2t, 2t + 1 and 2t + 8, 2t + 9.
-      // A q that holds no number makes its logits NaN here (the e4m3 conversion would make infinities finite).
-      const bool odd = (G == 4) && (t & 1);
-      float a = odd ? sums[G - 2] : sums[0], b = odd ? sums[G - 1] : sums[1];
-      float whole = 0.0f;
+      // (A q that holds an infinity or a NaN has one in its sums: its logits are none either.)
+      const bool high = (G == 4) && (t & 1);
 #pragma unroll
-      for (int g = 0; g < G; ++g) whole += sums[g];
-      uint32_t term[3];
+      for (int k = 0; k < 2; ++k) {
+        float a = k == 0 ? (high ? sums[G - 2] : sums[0]) : (high ? odds[G - 2] : odds[0]);
+        float b = k == 0 ? (high ? sums[G - 1] : sums[1]) : (high ? odds[G - 1] : odds[1]);
+        uint32_t term[3];
 #pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        term[i] = pack_bf16(a, b);
-        a -= bf16_lo(term[i]);
-        b -= bf16_hi(term[i]);
+        for (int i = 0; i < 3; ++i) {
+          term[i] = pack_bf16(a, b);
+          a -= bf16_lo(term[i]);
+          b -= bf16_hi(term[i]);
+        }
+        uint32_t* const to = k == 0 ? qz[nt] : qs[nt];
+        if (G == 4) {
+          to[0] = t < 2 ? term[0] : term[1];
+          to[1] = t < 2 ? term[2] : 0u;
+        } else {
+          to[0] = t == 0 ? term[0] : t == 1 ? term[1] : t == 2 ? term[2] : 0u;
+          to[1] = 0u;
+        }
       }
-      if (!(fabsf(whole) < INFINITY)) term[0] = term[1] = term[2] = 0x7fff7fffu;
-      if (G == 4) {
-        qz[nt][0] = t < 2 ? term[0] : term[1];
-        qz[nt][1] = t < 2 ? term[2] : 0u;
-      } else {
-        qz[nt][0] = t == 0 ? term[0] : t == 1 ? term[1] : t == 2 ? term[2] : 0u;
-        qz[nt][1] = 0u;
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) qs[nt][i] = pack_bf16(-8.0f * bf16_lo(qz[nt][i]), -8.0f * bf16_hi(qz[nt][i]));
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         cs[nt][j] = __shfl_sync(~0u, back, (2 * t + j) * 4);
@@ -448,13 +428,14 @@ struct Wide {
       }
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        const uint32_t a0 = kw[0][g] & 0x0f0f0f0fu, a1 = kw[1][g] & 0x0f0f0f0fu;
-        const uint32_t a2 = (kw[0][g] >> 4) & 0x0f0f0f0fu, a3 = (kw[1][g] >> 4) & 0x0f0f0f0fu;
+        uint32_t u0[4], u1[4];
+        unpack8<false>(consts, kw[0][g], u0);
+        unpack8<false>(consts, kw[1][g], u1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          mma_e4m3(a, a0, a1, a2, a3, qf[nt][g][0], qf[nt][g][1]);
-          mma_e4m3(a, a0, a1, a2, a3, qf[nt][g][2], qf[nt][g][3]);
+          mma_f16(a, u0[0], u1[0], u0[1], u1[1], qf[nt][g][0], qf[nt][g][1]);
+          mma_f16(a, u0[2], u1[2], u0[3], u1[3], qf[nt][g][2], qf[nt][g][3]);
           sacc[hf][nt][0] = fmaf(ks[0][g], a[0], sacc[hf][nt][0]);
           sacc[hf][nt][1] = fmaf(ks[0][g], a[1], sacc[hf][nt][1]);
           sacc[hf][nt][2] = fmaf(ks[1][g], a[2], sacc[hf][nt][2]);
@@ -623,7 +604,7 @@ struct Wide {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t u[4];
-          unpack8(consts, ww[i], u);
+          unpack8<true>(consts, ww[i], u);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
             mma_f16(o[nt][4 * a + i], u[0], u[1], u[2], u[3], pv[nt][2 * a + (i >> 1)][0], pv[nt][2 * a + (i >> 1)][1]);
@@ -666,21 +647,18 @@ struct Wide {
   }
 };
 
-// The same for one or two query rows (one query token, a K / V head to each query head or two): the 8 columns are the 4
-// groups of 32 channels times 2, so a lane deals with one group - column 2t, 2t + 1: group t - and with a quarter of the
-// scales, centres and products that the layout above gives every lane.  The second index of a column is the row, or, with
-// one row, the term of q for the logits.  With 64 channels there are two groups, and columns of the other half hold the
-// second term.  A column's product with another group's channels is zero (logits: its operand is) or not used (out).
+// The same for one or two query rows (one query token, a K / V head to each query head or two): the 8 columns are the groups of
+// 32 channels times two rows, so a lane deals with one group - columns 2t, 2t + 1: group t - and with a quarter of the
+// scales, centres and products that the layout above gives every lane.  (64 channels have two groups: the other half of the columns
+// is a copy.)  A column's product with another group's channels is zero (logits: its operand is) or not used (out).
 template <int D, int R>
 struct Narrow {
   using C = Chunk<D>;
   static constexpr int kD = D, G = D / 32, kTiles = D / 16, kRows = R;
   static constexpr int kWarps = NARROW_WARPS, kStages = NARROW_STAGES * (128 / D);
-  static constexpr int kTerms = D == 128 && R == 2 ? 2 : 1;   // instructions per group: the terms of q that have no column of their own
-  static constexpr bool kPairSum = D == 128 && R == 1;        // the two columns of a lane are the terms of one row
 
-  uint32_t qf[G][kTerms][2];    // q as the second operand, zero outside the column's group
-  float qs[R], q8[2];           // the sum of q over this lane's group; -8 times it for its columns (zero for second terms)
+  uint32_t qf[G][4];            // q as the second operand, zero outside the column's group: [2 m + {0, 1}], odd channels over 16
+  float qs[R], qo[2];           // sums of q over this lane's group, and over its odd channels times -72, of its columns
   float cs[R], m[R], l[R], oz[R];
   float o[kTiles][4];
   float vs_mul;
@@ -720,50 +698,33 @@ struct Narrow {
     top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
     top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
     top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
-    const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);   // largest member to [2^7, 2^8)
-    const float up = __uint_as_float(static_cast<uint32_t>(127 + 7 - e) << 23);
-    const float back = __uint_as_float(static_cast<uint32_t>(127 - 7 + e) << 23) * (512.0f * p.scale_log2e);   // (codes are 2^-9 c)
+    const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);   // largest member to [2^14, 2^15)
+    const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
+    const float back = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * p.scale_log2e;
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] *= up;
-    float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+    float odd = (f[1] + f[3]) + (f[5] + f[7]), sum = odd + ((f[0] + f[2]) + (f[4] + f[6]));
     sum += __shfl_xor_sync(~0u, sum, 1);
     sum += __shfl_xor_sync(~0u, sum, 2);
-    uint32_t term[2][2];
+    odd += __shfl_xor_sync(~0u, odd, 1);
+    odd += __shfl_xor_sync(~0u, odd, 2);
+    const bool used = R == 2 || (n & 1) == 0;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t v = (i & 1) ? pack_f16(f[i] * 0.0625f, f[i + 4] * 0.0625f) : pack_f16(f[i], f[i + 4]);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {   // word h: channels h, h + 2, h + 4, h + 6 (the codes in the low / high halves of a word's bytes)
-        const uint32_t b01 = pack_e4m3(f[h], f[h + 2]), b23 = pack_e4m3(f[h + 4], f[h + 6]);
-        term[k][h] = b01 | (b23 << 16);
-        float x0, x1, x2, x3;
-        unpack_e4m3(b01, x0, x1);
-        unpack_e4m3(b23, x2, x3);
-        f[h] -= x0; f[h + 2] -= x1; f[h + 4] -= x2; f[h + 6] -= x3;
-      }
-    // the term a column holds: with kTerms == 2 both, by turns; else by its place
-    const int second = kPairSum ? n & 1 : n >> 2;
-    const bool unused = D == 64 && R == 1 && (n & 1);
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-      for (int k = 0; k < kTerms; ++k)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t v = kTerms == 2 ? term[k][h] : second ? term[1][h] : term[0][h];
-          qf[g][k][h] = g == group && !unused ? v : 0u;
-        }
-    // to the lanes that own the columns' products.  A q that holds no number makes its logits NaN here.
+      for (int g = 0; g < G; ++g) qf[g][i] = g == group && used ? v : 0u;
+    }
+    // to the lanes that own the columns' products
+    qo[1] = 0.0f;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       const int from = (2 * t + j) * 4;
-      const float s = __shfl_sync(~0u, sum, from) * (1.0f / 512.0f);
+      qs[j] = __shfl_sync(~0u, sum, from);
+      qo[j] = -72.0f * __shfl_sync(~0u, odd, from);
       cs[j] = __shfl_sync(~0u, back, from);
-      const bool first_term = D == 128 || t < 2;
-      qs[j] = !(fabsf(s) < INFINITY) ? __uint_as_float(0x7fffffffu) : first_term ? s : 0.0f;
-      q8[j] = -8.0f * qs[j];
       l[j] = 0.0f; m[j] = kNone; oz[j] = 0.0f;
     }
-    if (R == 1) q8[1] = 0.0f;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
@@ -781,7 +742,7 @@ struct Narrow {
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       const uint32_t c = c0 + hf * C::kBytes;
-      float a[4] = {q8[0], q8[1], q8[0], q8[1]};
+      float a[4] = {qo[0], qo[1], qo[0], qo[1]};
       uint32_t kw[2][G];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -796,10 +757,11 @@ struct Narrow {
       }
 #pragma unroll
       for (int i = 0; i < G; ++i) {
-        const uint32_t a0 = kw[0][i] & 0x0f0f0f0fu, a1 = kw[1][i] & 0x0f0f0f0fu;
-        const uint32_t a2 = (kw[0][i] >> 4) & 0x0f0f0f0fu, a3 = (kw[1][i] >> 4) & 0x0f0f0f0fu;
-#pragma unroll
-        for (int k = 0; k < kTerms; ++k) mma_e4m3(a, a0, a1, a2, a3, qf[i][k][0], qf[i][k][1]);
+        uint32_t u0[4], u1[4];
+        unpack8<false>(consts, kw[0][i], u0);
+        unpack8<false>(consts, kw[1][i], u1);
+        mma_f16(a, u0[0], u1[0], u0[1], u1[1], qf[i][0], qf[i][1]);
+        mma_f16(a, u0[2], u1[2], u0[3], u1[3], qf[i][2], qf[i][3]);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -807,8 +769,7 @@ struct Narrow {
         const float ks = bf16_lo(lds16(cz)), kz = bf16_lo(lds16(cz + 2 * G));
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-          const float x = kPairSum ? a[2 * h] + a[2 * h + 1] : a[2 * h + j];
-          s[hf][h][j] = fmaf(ks, x, kz * qs[j]);
+          s[hf][h][j] = fmaf(ks, a[2 * h + j], kz * qs[j]);
         }
         vsb[hf][h] = lds16(c + C::kVs + (r + 8 * h) * (2 * G) + 2 * g);
         vz[hf][h] = bf16_lo(lds16(c + C::kVz + g * 32 + (r + 8 * h) * 2));
@@ -821,7 +782,7 @@ struct Narrow {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
           s[hf][h][j] += __shfl_xor_sync(~0u, s[hf][h][j], 1);
-          s[hf][h][j] += __shfl_xor_sync(~0u, s[hf][h][j], 2);
+          if (G == 4) s[hf][h][j] += __shfl_xor_sync(~0u, s[hf][h][j], 2);
         }
     if (gone != 0 || key0 + 2 * kChunkTokens > least) {
       // hidden keys: logits at -inf, and nothing of bytes that were never written
@@ -916,7 +877,7 @@ struct Narrow {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t u[4];
-          unpack8(consts, ww[i], u);
+          unpack8<true>(consts, ww[i], u);
           mma_f16(o[4 * a + i], u[0], u[1], u[2], u[3], pv[0], pv[1]);
         }
       }
@@ -1033,15 +994,30 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
         *reinterpret_cast<uint4*>(p.out + s * out_seq + i * 8) = make_uint4(0, 0, 0, 0);
   if (carry == 0) return;
 
-  // This CTA's part of the line.  Where every unit can have a CTA of its own and no warp then gets more than four chunks, it has:
-  // nothing is joined across CTAs (one request, 32 heads, 640 keys: 8.6 us against 12.3).
+  // This CTA's part of the line: an equal one, except that
+  //   - where every unit can have a CTA of its own and no warp then gets more than four chunks, it has: nothing is joined across CTAs
+  //     (one request, 32 heads, 640 keys: 7.5 us against 12.3);
+  //   - where a part is at least four times the longest unit, its ends move to the nearest unit's, for the same reason (64 requests of
+  //     200 to 1800 keys: JOINED against 83 us).
   const long long total = static_cast<long long>(carry) * units_per_seq;
   const Cut cut = cut_of(total, gridDim.x);
   const bool own_unit = static_cast<long long>(p.n_seq) * units_per_seq <= gridDim.x && longest <= 4 * kWarps;
+  const bool whole_units = own_unit || cut.per / 4 >= longest;
   auto unit_begin = [&](int unit, int* n) {
     const int seq = unit / units_per_seq;
     *n = first[seq + 1] - first[seq];
     return static_cast<long long>(first[seq]) * units_per_seq + static_cast<long long>(unit - seq * units_per_seq) * *n;
+  };
+  // the sequence that has place x of the line (x < total): first[s] * units <= x < first[s + 1] * units
+  auto seq_of = [&](long long x) {
+    int lo = 0;
+    for (int n = p.n_seq; n > 1;) {          // among sequences lo .. lo + n - 1; a step of 32 ways
+      const int width = (n + 31) / 32, s = lo + (lane + 1) * width;
+      const int past = __popc(__ballot_sync(~0u, (lane + 1) * width < n && static_cast<long long>(first[s]) * units_per_seq <= x));
+      lo += past * width;
+      n = min(width, n - past * width);
+    }
+    return lo;
   };
   long long line0, line1;
   if (own_unit) {
@@ -1053,6 +1029,16 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
     if (static_cast<int>(blockIdx.x) >= cut.ctas) return;
     line0 = cut.begin(blockIdx.x);
     line1 = cut.begin(blockIdx.x + 1);
+    if (whole_units) {
+      auto nearest = [&](long long x) {
+        if (x == total) return x;
+        const int s = seq_of(x), n = first[s + 1] - first[s];
+        const long long base = static_cast<long long>(first[s]) * units_per_seq;
+        return base + Cut::divide(x - base + n / 2, n) * n;
+      };
+      line0 = nearest(line0);
+      line1 = nearest(line1);
+    }
   }
   if (line0 == line1) return;
   // Its warps share it by pairs of chunks.
@@ -1063,11 +1049,7 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
     Cursor at;       // where the warp computes
     {
       const long long begin = warp_begin(warp);
-      int lo = 0, hi = p.n_seq - 1;          // the sequence with first[s] * units <= begin < first[s + 1] * units
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (static_cast<long long>(first[mid + 1]) * units_per_seq <= begin) lo = mid + 1; else hi = mid;
-      }
+      const int lo = seq_of(begin);
       const long long rem = begin - static_cast<long long>(first[lo]) * units_per_seq;
       const int n = first[lo + 1] - first[lo];
       const int unit = static_cast<int>(Cut::divide(rem, n));
@@ -1178,9 +1160,10 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   }
 
   // ---------------------------------------------------------------- joining
-  // A unit whose parts are all in this CTA gets its output; of the others - at most the one the CTA begins in and the one it
-  // ends in - the CTA leaves one part for the CTA that comes last.  Parts of a unit: the last one of the warp it begins in (none,
-  // if it began before the CTA), then the first ones of the warps that follow.
+  // Parts of a unit in this CTA: the last one of the warp it begins in (none, if it began before the CTA), then the first ones of
+  // the warps that follow.  With few rows a warp joins the unit that begins in it, warp 0 also the one that began before the CTA; with
+  // more, or where the CTA has parts of one unit only, the warps share the rows of one unit after the other.  A unit whose parts are all here gets its output; of the others - at most the one
+  // the CTA begins in and the one it ends in - the CTA leaves one part for the CTA that comes last.
   __syncthreads();
   auto write_out = [&](int unit, int in_tile, const RowSum& s) {
     const int seq = unit / units_per_seq, u = unit - seq * units_per_seq;
@@ -1191,27 +1174,32 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
           make_uint2(pack_bf16(s.v.x * inv, s.v.y * inv), pack_bf16(s.v.z * inv, s.v.w * inv));
   };
   auto rows_of = [&](int unit) { return p.tiles == 1 ? p.rows : min(kRows, p.rows - (unit % p.tiles) * kRows); };
-  int open[2] = {-1, -1};           // units of the parts this CTA leaves: that began before it, that begins in it
+  int open[2];                      // units of the parts this CTA leaves: that began before it, that begins in it; -1: none
   {
     const int heads = lane < kWarps ? part_unit[lane][0] : -1, tails = lane < kWarps ? part_unit[lane][1] : -1;
-    uint32_t begins = __ballot_sync(~0u, tails >= 0) << 1 | (__shfl_sync(~0u, heads, 0) >= 0 ? 1u : 0u);   // bit w + 1: a unit begins in warp w
-    int task = 0;
-    while (begins != 0) {
-      const int w = __ffs(begins) - 2;          // -1: it began before the CTA
-      begins &= begins - 1;
-      const int unit = w < 0 ? __shfl_sync(~0u, heads, 0) : __shfl_sync(~0u, tails, w);
-      const uint32_t in = __ballot_sync(~0u, heads == unit);
-      const int lead = w >= 0 ? 1 : 0, n = lead + __popc(in), w1 = in != 0 ? __ffs(in) - 1 : 0;
+    const uint32_t begun = __ballot_sync(~0u, tails >= 0);         // warps in which a unit begins that they leave unfinished
+    open[0] = __shfl_sync(~0u, heads, 0);
+    open[1] = begun != 0 ? __shfl_sync(~0u, tails, 31 - __clz(begun)) : -1;
+    if (open[1] >= 0) {
       int chunks;
-      const bool here = unit_begin(unit, &chunks) + chunks <= line1 && w >= 0;
-      if (!here) open[lead] = unit;
+      if (unit_begin(open[1], &chunks) + chunks <= line1) open[1] = -1;
+    }
+    const bool shared = kRows > 2 || __popc(begun) + (open[0] >= 0 ? 1 : 0) == 1;
+    // bit w + 1: join the unit that begins in warp w; bit 0: the one that began before the CTA
+    uint32_t mine = (shared ? begun << 1 : begun & (1u << warp) ? 2u << warp : 0u) | ((shared || warp == 0) && open[0] >= 0 ? 1u : 0u);
+    for (; mine != 0; mine &= mine - 1) {
+      const int w = __ffs(mine) - 2, lead = w >= 0 ? 1 : 0;
+      const int unit = lead == 0 ? open[0] : __shfl_sync(~0u, tails, w);
+      const uint32_t in = __ballot_sync(~0u, heads == unit);
+      const int n = lead + __popc(in), w1 = w + 1;
+      const bool leave = unit == open[lead];
       const int rows = rows_of(unit);
-      for (int row = (warp + kWarps - task % kWarps) % kWarps; row < rows; row += kWarps) {
+      for (int row = shared ? warp : 0; row < rows; row += shared ? kWarps : 1) {
         const RowSum s = join_row<D, false>(n, [&](int k) {
           const int at = k < lead ? w * Sh::kWarpRing : Sh::kHeads + (w1 + k - lead) * Sh::kHeadPart;
           return reinterpret_cast<const float*>(smem + at) + row * kPart;
         }, lane);
-        if (here) {
+        if (!leave) {
           write_out(unit, row, s);
         } else {
           float* const to = p.part + static_cast<size_t>((2 * blockIdx.x + lead) * p.part_rows + row) * kPart;
@@ -1219,7 +1207,6 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
           if (lane == 0) *reinterpret_cast<float2*>(to) = make_float2(s.m, s.l);
         }
       }
-      task += rows;
     }
   }
   if (open[0] < 0 && open[1] < 0) return;
