@@ -313,6 +313,28 @@ class PageConfig:
         self.ref = ctypes.addressof(c)
 
 
+def _page_call(name):
+    """The C entry point, and a caller for tensors: a decoded token is three calls of a few microseconds of GPU time, so their
+    arguments go straight through (integers and None too, as everywhere)."""
+    f = getattr(lib(), "mustdrop_page_" + name)
+    import torch
+    raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    device = torch.cuda.current_device
+
+    def call(config, stream, *buffers):
+        if stream is None and raw_stream is not None:
+            stream = raw_stream(device())
+        elif not isinstance(stream, int):
+            stream = _stream(stream)
+        return f(config.ref, *[b.data_ptr() if hasattr(b, "data_ptr") else b for b in buffers], stream)
+
+    _page_calls[name] = call
+    return call
+
+
+_page_calls = {}
+
+
 def mustdrop_page_pool_bytes(config: PageConfig) -> int:
     return lib().mustdrop_page_pool_bytes(config.ref)
 
@@ -323,24 +345,20 @@ def mustdrop_page_workspace_bytes(config: PageConfig) -> int:
 
 def mustdrop_page_tables(config: PageConfig, add, len, ring_state, len_out, ring_state_out, ring, page_table, slots,
                          workspace, stream=None) -> int:
-    return lib().mustdrop_page_tables(config.ref, _ptr(add), _ptr(len), _ptr(ring_state), _ptr(len_out),
-                                      _ptr(ring_state_out), _ptr(ring), _ptr(page_table), _ptr(slots), _ptr(workspace),
-                                      _stream(stream))
+    return (_page_calls.get("tables") or _page_call("tables"))(
+        config, stream, add, len, ring_state, len_out, ring_state_out, ring, page_table, slots, workspace)
 
 
 def mustdrop_page_store(config: PageConfig, slots, k, v, pool, workspace=None, stream=None) -> int:
-    return lib().mustdrop_page_store(config.ref, _ptr(slots), _ptr(k), _ptr(v), _ptr(pool), _ptr(workspace),
-                                     _stream(stream))
+    return (_page_calls.get("store") or _page_call("store"))(config, stream, slots, k, v, pool, workspace)
 
 
 def mustdrop_page_load(config: PageConfig, slots, pool, k_out, v_out, workspace=None, stream=None) -> int:
-    return lib().mustdrop_page_load(config.ref, _ptr(slots), _ptr(pool), _ptr(k_out), _ptr(v_out), _ptr(workspace),
-                                    _stream(stream))
+    return (_page_calls.get("load") or _page_call("load"))(config, stream, slots, pool, k_out, v_out, workspace)
 
 
 def mustdrop_page_attend(config: PageConfig, q, pool, page_table, len, out, workspace, stream=None) -> int:
-    return lib().mustdrop_page_attend(config.ref, _ptr(q), _ptr(pool), _ptr(page_table), _ptr(len), _ptr(out),
-                                      _ptr(workspace), _stream(stream))
+    return (_page_calls.get("attend") or _page_call("attend"))(config, stream, q, pool, page_table, len, out, workspace)
 
 
 def mustdrop_plan_describe(plan) -> str:

@@ -29,10 +29,10 @@ namespace {
 // A pure function of the lengths: with need[s] = pages sequence s asks for, back[s] = pages it gives back, P the
 // sums over the sequences before it, its i-th new page is ring[head + P_need + i] and its i-th returned page goes to
 // ring[head + count + P_back + i].  The ring's two ends never meet (count + all of back <= n_pages), so no CTA
-// waits for another: each sums need and back over the sequences before its own (two loads per sequence, from
-// L2), handles its own ones, and the CTA that finishes last writes what the others still read - the ring's state and, as
-// they may be updated in place, the lengths.  Bound: launch and three dependent trips to L2 for small calls,
-// the slots written for large ones.
+// waits for another: each sums need and back over the sequences before its own (two loads per sequence, from L2) and
+// handles its own ones.  What the others still read - lengths and state that are updated in place - is written by the CTA that finishes
+// last; one CTA alone, or outputs of their own, need no such order.  Bound: launch and three dependent trips to L2
+// (240 sequences, one token: TAB1 us, where an empty kernel takes 2.3), the slots written for large calls.
 struct TableParams {
   const int32_t *add, *len, *state;
   int32_t *len_out, *state_out, *ring, *table, *slots;
@@ -44,7 +44,7 @@ constexpr int kTableThreads = 512;
 constexpr int kTableSeqs = 1024;     // most sequences of a CTA
 
 struct Move {       // what the call does to one sequence
-  int32_t cur, grow, need, back;   // grow: tokens gained (0 where it shrinks or is refused for its length)
+  int32_t cur, grow, need, back, left;   // grow: tokens gained (0 where it shrinks or is refused for its length); left: tokens it then has
   bool bad;
 };
 
@@ -52,37 +52,37 @@ __device__ __forceinline__ Move move_of(const TableParams& p, int s) {
   Move m;
   m.cur = p.len[s];
   const int32_t a = p.add[s];
-  const int64_t most = static_cast<int64_t>(p.max_pages) << p.lg;
-  const int32_t mask = (1 << p.lg) - 1;
+  const int32_t most = p.max_pages << p.lg, mask = (1 << p.lg) - 1;
+  const int64_t to = static_cast<int64_t>(m.cur) + a;
   m.grow = m.need = m.back = 0;
-  m.bad = m.cur < 0 || m.cur > most || a > p.rows || m.cur + static_cast<int64_t>(a) > most;
+  m.left = m.cur;
+  m.bad = m.cur < 0 || m.cur > most || a > p.rows || to > most;
   if (m.bad) return m;
-  const int32_t had = static_cast<int32_t>((static_cast<int64_t>(m.cur) + mask) >> p.lg);
-  if (a >= 0) {
-    m.grow = a;
-    m.need = static_cast<int32_t>((static_cast<int64_t>(m.cur) + a + mask) >> p.lg) - had;
-  } else {
-    const int64_t left = max(static_cast<int64_t>(m.cur) + a, static_cast<int64_t>(0));
-    m.back = had - static_cast<int32_t>((left + mask) >> p.lg);
-  }
+  m.left = static_cast<int32_t>(to < 0 ? 0 : to);
+  const int32_t had = static_cast<int32_t>((static_cast<uint32_t>(m.cur) + mask) >> p.lg);
+  const int32_t pages = static_cast<int32_t>((static_cast<uint32_t>(m.left) + mask) >> p.lg);
+  m.grow = max(a, 0);
+  m.need = max(pages - had, 0);
+  m.back = max(had - pages, 0);
   return m;
 }
 
-// Inclusive sums of (x, y) over the CTA's threads; `total` receives the sums over all.  Ends with a barrier passed.
-__device__ __forceinline__ longlong2 scan_pair(longlong2 v, longlong2* warp_sums, longlong2* total) {
+// Inclusive sums of (x, y) over the CTA's threads (they fit 32 bits: the page table has fewer than 2^31 entries);
+// `total` receives the sums over all.
+__device__ __forceinline__ int2 scan_pair(int2 v, int2* warp_sums, int2* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const long long x = __shfl_up_sync(~0u, v.x, d), y = __shfl_up_sync(~0u, v.y, d);
+    const int x = __shfl_up_sync(~0u, v.x, d), y = __shfl_up_sync(~0u, v.y, d);
     if (lane >= d) { v.x += x; v.y += y; }
   }
   __syncthreads();
   if (lane == 31) warp_sums[warp] = v;
   __syncthreads();
-  longlong2 all = {0, 0};
+  int2 all = {0, 0};
 #pragma unroll
   for (int w = 0; w < kTableThreads / 32; ++w) {
-    const longlong2 t = warp_sums[w];
+    const int2 t = warp_sums[w];
     if (w < warp) { v.x += t.x; v.y += t.y; }
     all.x += t.x; all.y += t.y;
   }
@@ -90,46 +90,60 @@ __device__ __forceinline__ longlong2 scan_pair(longlong2 v, longlong2* warp_sums
   return v;
 }
 
+// Place i (below 2 n_pages) of the ring.
+__device__ __forceinline__ int32_t in_ring(const TableParams& p, int32_t i) { return i < p.n_pages ? i : i - p.n_pages; }
+
 __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams p) {
-  __shared__ longlong2 warp_sums[kTableThreads / 32];
+  __shared__ int2 warp_sums[kTableThreads / 32];
   __shared__ int32_t cur_s[kTableSeqs], grow_s[kTableSeqs], first_s[kTableSeqs];   // first_s: ring offset of the first new page
   __shared__ int32_t back_s[kTableSeqs], back_at_s[kTableSeqs];                    // pages given back, and their place behind the ring's count
+  __shared__ int32_t left_s[kTableSeqs];                                           // the new length
   __shared__ int last_s;
   pdl_launch_dependents();
   pdl_wait();
   const int first = blockIdx.x * p.per_cta, n_own = min(p.per_cta, p.n_seq - first);
   int32_t head = p.state[0], count = p.state[1];
+  const int32_t given_head = head, given_count = count;
   const bool bad_state = head < 0 || head >= p.n_pages || count < 0 || count > p.n_pages;
   if (bad_state) head = count = 0;   // nothing is free, nothing can be given back
-  longlong2 before = {0, 0}, total;
-  for (int s = threadIdx.x; s < first; s += kTableThreads) {
-    const Move m = move_of(p, s);
-    before.x += m.need; before.y += m.back;
-  }
+  int2 before = {0, 0}, total;
   if (first > 0) {
-    (void)scan_pair(before, warp_sums, &total);
-    before = total;
+#pragma unroll 4
+    for (int s = threadIdx.x; s < first; s += kTableThreads) {
+      const Move m = move_of(p, s);
+      before.x += m.need; before.y += m.back;
+    }
+    before.x = __reduce_add_sync(~0u, before.x);
+    before.y = __reduce_add_sync(~0u, before.y);
+    if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5] = before;
+    __syncthreads();
+    before = {0, 0};
+#pragma unroll
+    for (int w = 0; w < kTableThreads / 32; ++w) { before.x += warp_sums[w].x; before.y += warp_sums[w].y; }
   }
+  int32_t taken = 0;                   // largest sum of pages asked for that is granted, among this thread's sequences
   const bool lead = blockIdx.y == 0;   // of the CTAs that share a range of sequences, the one that reports
   for (int base = 0; base < n_own; base += kTableThreads) {
     const int i = base + threadIdx.x, s = first + i;
-    Move m = {0, 0, 0, 0, false};
+    Move m = {0, 0, 0, 0, 0, false};
     if (i < n_own) m = move_of(p, s);
-    longlong2 upto = scan_pair({m.need, m.back}, warp_sums, &total);
+    int2 upto = scan_pair({m.need, m.back}, warp_sums, &total);
     upto.x += before.x; upto.y += before.y;
     before.x += total.x; before.y += total.y;
     if (i < n_own) {
       const bool granted = m.need == 0 || upto.x <= count;
+      if (granted && m.need > 0) taken = max(taken, upto.x);
       cur_s[i] = m.cur;
       grow_s[i] = granted ? m.grow : 0;
-      first_s[i] = granted && m.need > 0 ? static_cast<int32_t>(upto.x - m.need) : 0;
+      left_s[i] = granted ? m.left : m.cur;
+      first_s[i] = granted && m.need > 0 ? upto.x - m.need : 0;
       if (lead && m.bad) record_status(p.workspace, MUSTDROP_ERR_BAD_LENGTH, s);
       if (lead && !granted) record_status(p.workspace, MUSTDROP_ERR_NO_PAGES, s);
       // what does not fit behind the ring's count was never the pool's
-      const long long room = bad_state ? 0 : max(static_cast<long long>(p.n_pages) - count - (upto.y - m.back), 0ll);
+      const int32_t room = bad_state ? 0 : max(p.n_pages - count - (upto.y - m.back), 0);
       if (lead && m.back > room) record_status(p.workspace, MUSTDROP_ERR_BAD_LENGTH, s);
-      back_s[i] = static_cast<int32_t>(min(static_cast<long long>(m.back), room));
-      back_at_s[i] = static_cast<int32_t>(back_s[i] > 0 ? count + (upto.y - m.back) : 0);
+      back_s[i] = min(m.back, room);
+      back_at_s[i] = back_s[i] > 0 ? count + (upto.y - m.back) : 0;
     }
   }
   __syncthreads();
@@ -137,13 +151,12 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
   for (int i = threadIdx.x >> 5; lead && i < n_own; i += kTableThreads / 32) {
     const int n = back_s[i];
     if (n == 0) continue;
-    const Move m = move_of(p, first + i);
-    const int32_t had = static_cast<int32_t>((static_cast<int64_t>(m.cur) + (1 << p.lg) - 1) >> p.lg);
-    const int32_t* from = p.table + static_cast<size_t>(first + i) * p.max_pages + (had - m.back);
+    const int32_t pages = static_cast<int32_t>((static_cast<uint32_t>(left_s[i]) + (1 << p.lg) - 1) >> p.lg);
+    const int32_t* from = p.table + static_cast<size_t>(first + i) * p.max_pages + pages;
     for (int b = threadIdx.x & 31; b < n; b += 32) {
       const int32_t id = from[b];
       if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.n_pages)) record_status(p.workspace, MUSTDROP_ERR_BAD_PAGE, first + i);
-      p.ring[(static_cast<int64_t>(head) + back_at_s[i] + b) % p.n_pages] = id;
+      p.ring[in_ring(p, in_ring(p, head + back_at_s[i]) + b)] = id;
     }
   }
   // slots, and the table entries of the pages that begin among the new tokens
@@ -159,7 +172,7 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
       int32_t* row = p.table + static_cast<size_t>(first + i) * p.max_pages;
       const int32_t cur = cur_s[i], pos = cur + r, e = pos >> p.lg;
       const int32_t had = static_cast<int32_t>((static_cast<uint32_t>(cur) + mask) >> p.lg);
-      const int32_t id = e < had ? row[e] : p.ring[(static_cast<int64_t>(head) + first_s[i] + (e - had)) % p.n_pages];
+      const int32_t id = e < had ? row[e] : p.ring[in_ring(p, head + first_s[i] + (e - had))];
       if (e >= had && (pos & mask) == 0) row[e] = id;
       if (static_cast<uint32_t>(id) < static_cast<uint32_t>(p.n_pages)) slot = (id << p.lg) | (pos & mask);
       else record_status(p.workspace, MUSTDROP_ERR_BAD_PAGE, first + i);
@@ -168,51 +181,61 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
     i += di; t += dt;
     if (t >= n_t) { t -= n_t; ++i; }
   }
-  // the CTA that finishes last: everybody has read what it now overwrites
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    const unsigned all = gridDim.x * gridDim.y;
-    last_s = all == 1 || atomicInc(reinterpret_cast<unsigned*>(p.workspace) + kTicketWord, all - 1) == all - 1;
-    __threadfence();
-  }
-  __syncthreads();
-  if (!last_s) return;
-  longlong2 sum = {0, 0};
-  long long taken = 0;
-  for (int base = 0; base < p.n_seq; base += kTableThreads) {
-    const int s = base + threadIdx.x;
-    Move m = {0, 0, 0, 0, false};
-    int32_t a = 0;
-    if (s < p.n_seq) {
-      m = move_of(p, s);
-      a = p.add[s];
+  // Lengths and state.  Every CTA has read all of them that lie before its own, so what is updated in place waits for the CTA
+  // that finishes last.
+  const unsigned all = gridDim.x * gridDim.y;
+  const bool in_place = p.len_out == p.len || p.state_out == p.state;
+  const bool at_end = first + n_own == p.n_seq;
+  bool mine = at_end && lead;          // this CTA writes the state
+  if (in_place && all > 1) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      __threadfence();
+      last_s = atomicInc(reinterpret_cast<unsigned*>(p.workspace) + kTicketWord, all - 1) == all - 1;
+      __threadfence();
     }
-    longlong2 upto = scan_pair({m.need, m.back}, warp_sums, &total);
-    upto.x += sum.x;
-    sum.x += total.x; sum.y += total.y;
-    if (s < p.n_seq) {
-      const bool granted = m.need == 0 || upto.x <= count;
-      if (granted && m.need > 0) taken = max(taken, upto.x);
-      p.len_out[s] = m.bad ? m.cur : a < 0 ? max(m.cur + a, 0) : granted ? m.cur + m.grow : m.cur;
+    __syncthreads();
+    if (!last_s) return;
+    mine = true;
+  } else if (lead) {
+    for (int k = threadIdx.x; k < n_own; k += kTableThreads) p.len_out[first + k] = left_s[k];
+  }
+  if (!mine) return;
+  // A second walk over all sequences where this CTA has to write their lengths, or has not seen which were granted.
+  if (all > 1 && (in_place || before.x > count)) {
+    before = {0, 0};
+    taken = 0;
+    for (int base = 0; base < p.n_seq; base += kTableThreads) {
+      const int s = base + threadIdx.x;
+      Move m = {0, 0, 0, 0, 0, false};
+      if (s < p.n_seq) m = move_of(p, s);
+      int2 upto = scan_pair({m.need, m.back}, warp_sums, &total);
+      upto.x += before.x;
+      before.x += total.x; before.y += total.y;
+      if (s < p.n_seq) {
+        const bool granted = m.need == 0 || upto.x <= count;
+        if (granted && m.need > 0) taken = max(taken, upto.x);
+        if (in_place) p.len_out[s] = granted ? m.left : m.cur;
+      }
     }
   }
-  // the granted needs are those up to the largest sum that fits
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) taken = max(taken, __shfl_xor_sync(~0u, taken, d));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5].x = taken;
-  __syncthreads();
-  if (threadIdx.x == 0) {
+  if (before.x <= count) {
+    taken = before.x;
+  } else {
+    taken = __reduce_max_sync(~0u, taken);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5].x = taken;
+    __syncthreads();
     for (int w = 0; w < kTableThreads / 32; ++w) taken = max(taken, warp_sums[w].x);
+  }
+  if (threadIdx.x == 0) {
     if (bad_state) {
       record_status(p.workspace, MUSTDROP_ERR_BAD_LENGTH, -1);
-      p.state_out[0] = p.state[0];
-      p.state_out[1] = p.state[1];
+      p.state_out[0] = given_head;
+      p.state_out[1] = given_count;
     } else {
-      const long long back = min(sum.y, static_cast<long long>(p.n_pages) - count);
-      p.state_out[0] = static_cast<int32_t>((head + taken) % p.n_pages);
-      p.state_out[1] = static_cast<int32_t>(count - taken + back);
+      p.state_out[0] = in_ring(p, head + taken);
+      p.state_out[1] = count - taken + min(before.y, p.n_pages - count);
     }
   }
 }
@@ -251,37 +274,70 @@ __device__ __forceinline__ uint32_t to_bf16(float x) {   // round to nearest eve
   return h;
 }
 
+__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {   // a NaN stays one
+  uint32_t d;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ bool finite_bf16(uint32_t bits) { return (bits & 0x7f80u) != 0x7f80u; }
+
 // Codes of eight channels as nibbles 0..7 of a word; scale and centre (bf16 bits) of the group of four lanes.
+//
+// A code is round((x - z) / s) + 8, ties to even.  With d = x - z (fp32) and the reciprocal of s in two fp32 terms, q = d hi +
+// d lo is d / s to 2^-47 before its one rounding.  That decides as the correctly rounded quotient does: a tie s (k + 1/2) has 13
+// bits, so another fp32 number d is more than 2^-24 of it away, which q's rounding keeps on its side; a tie itself is kept exactly.
+// (|d / s| stays below 32: where the centre's rounding is many steps, so is the spacing of bf16 numbers beside it.)  No division
+// and no conversion per channel: both run at a quarter of the rate of what is used here (the 32 x 192 x 32 rows of a pruned prompt: 71
+// us with them, STORED without).
 __device__ __forceinline__ uint32_t quantise8(const uint4& v, uint32_t* scale, uint32_t* centre) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  float x[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
-  float lo = x[0], hi = x[0];
-  bool finite = true;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]);
-    finite = finite && (__float_as_uint(x[i]) & 0x7f800000u) != 0x7f800000u;
-  }
+  uint32_t lo2 = min_bf16x2(min_bf16x2(w[0], w[1]), min_bf16x2(w[2], w[3]));
+  uint32_t hi2 = max_bf16x2(max_bf16x2(w[0], w[1]), max_bf16x2(w[2], w[3]));
 #pragma unroll
   for (int d = 1; d < 4; d <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(~0u, lo, d));
-    hi = fmaxf(hi, __shfl_xor_sync(~0u, hi, d));
-    finite = __shfl_xor_sync(~0u, static_cast<int>(finite), d) != 0 && finite;
+    lo2 = min_bf16x2(lo2, __shfl_xor_sync(~0u, lo2, d));
+    hi2 = max_bf16x2(hi2, __shfl_xor_sync(~0u, hi2, d));
   }
+  lo2 = min_bf16x2(lo2, lo2 >> 16 | lo2 << 16);
+  hi2 = max_bf16x2(hi2, hi2 >> 16 | hi2 << 16);
+  if (!finite_bf16(lo2) || !finite_bf16(hi2)) {   // (the centre stays finite: the attention multiplies it by zero for hidden keys)
+    *scale = 0x7fc0u;
+    *centre = 0;
+    return 0;
+  }
+  const float lo = bf16_lo(lo2), hi = bf16_lo(hi2);
   *scale = to_bf16(__fdiv_rn(__fsub_rn(0.5f * hi, 0.5f * lo), 7.5f));   // (halves: the difference of two finite numbers may not be one)
   const float s = __uint_as_float(*scale << 16);
   *centre = to_bf16(__fmaf_rn(8.0f, s, lo));
   const float z = __uint_as_float(*centre << 16);
+  if (s == 0.0f) return 0x88888888u;
+  if (s < 0x1p-100f) {   // a reciprocal whose second term would not be a normal number
+    uint32_t codes = 0;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+      const float x = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+      const float c = rintf(__fdiv_rn(__fsub_rn(x, z), s)) + 8.0f;
+      codes |= static_cast<uint32_t>(fminf(fmaxf(c, 0.0f), 15.0f)) << (4 * i);
+    }
+    return codes;
+  }
+  const float hi_inv = __frcp_rn(s), lo_inv = __fmul_rn(__fmaf_rn(-s, hi_inv, 1.0f), hi_inv);
+  constexpr float kMagic = 12582912.0f;     // 1.5 x 2^23: adding it rounds to a whole number, and its bits plus that number are the sum's
   uint32_t codes = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float c = s > 0.0f ? rintf(__fdiv_rn(__fsub_rn(x[i], z), s)) + 8.0f : 8.0f;
-    codes |= static_cast<uint32_t>(fminf(fmaxf(c, 0.0f), 15.0f)) << (4 * i);
+  for (int i = 7; i >= 0; --i) {
+    const float x = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+    const float d = __fsub_rn(x, z);
+    const float t = __fadd_rn(__fmaf_rn(d, hi_inv, __fmul_rn(d, lo_inv)), kMagic);
+    codes = codes * 16u + __float_as_uint(fminf(fmaxf(t, kMagic - 8.0f), kMagic + 7.0f));
   }
-  if (!finite) { *scale = 0x7fc0u; *centre = 0; codes = 0; }   // (the centre stays finite: the attention multiplies it by zero for hidden keys)
-  return codes;
+  // sum of 16^i (bits of kMagic + c_i - 8), c_i wanted
+  return codes - 0x11111111u * (0x4b400000u - 8u);
 }
 
 template <int D>
@@ -377,17 +433,17 @@ __global__ void __launch_bounds__(kRowThreads) page_store_kernel(RowParams p) {
   }
 }
 
-// Eight values z + s (c - 8), rounded to bf16.
+// Eight values z + s (c - 8), rounded to bf16: nibbles j and j + 4 as a bf16 pair 128 + c, less 136, and one fused operation.
 __device__ __forceinline__ uint4 values8(uint32_t codes, uint32_t scale, uint32_t centre) {
-  const float s = __uint_as_float(scale << 16), z = __uint_as_float(centre << 16);
-  uint32_t w[4];
+  const uint32_t s2 = scale | scale << 16, z2 = centre | centre << 16;
+  uint32_t v[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float lo = __fmaf_rn(s, static_cast<float>(static_cast<int>((codes >> (8 * i)) & 15u) - 8), z);
-    const float hi = __fmaf_rn(s, static_cast<float>(static_cast<int>((codes >> (8 * i + 4)) & 15u) - 8), z);
-    w[i] = to_bf16(lo) | (to_bf16(hi) << 16);
+  for (int j = 0; j < 4; ++j) {
+    uint32_t y = ((codes >> (4 * j)) & 0x000f000fu) | 0x43004300u;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(y), "r"(0x43084308u));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[j]) : "r"(y), "r"(s2), "r"(z2));
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  return make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
 }
 
 template <int D>
@@ -470,7 +526,8 @@ mustdrop_status_t mustdrop_page_tables(const mustdrop_page_config_t* c, const in
   const mustdrop_status_t st = check_page_sizes(c);
   if (st != MUSTDROP_OK) return st;
   if (c->rows <= 0 || c->max_pages <= 0) return MUSTDROP_ERR_INVALID_ARG;
-  if (static_cast<int64_t>(c->max_pages) * c->page > INT32_MAX) return MUSTDROP_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(c->max_pages) * c->page > INT32_MAX || static_cast<int64_t>(c->max_pages) * c->n_seq > INT32_MAX)
+    return MUSTDROP_ERR_UNSUPPORTED;
   if (workspace == nullptr) return MUSTDROP_ERR_WORKSPACE;
   const void* ints[] = {add, len, ring_state, len_out, ring_state_out, ring, page_table, slots};
   for (const void* q : ints)
