@@ -242,11 +242,13 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
 
 // ---------------------------------------------------------------------------------------- rows in, rows out
 //
-// A warp takes four rows of one head: 16 lanes hold a row of 128 channels (8 of 64) as 16-byte vectors, a lane two
-// rows (four).  A lane's eight channels are one word of the K codes; for V a word holds four tokens, so the lanes of
-// the four rows exchange their bytes and store whole words where the four slots are neighbours in one word, else single bytes.
-// Rows are grouped so that they are: groups of four end where slot mod 4 is 3, judged by the sequence's first slot.  Bound: bytes
-// (2 rows of bf16 in, a third as much out, and the reverse).
+// Store: a lane has one row's group of 32 channels (64 bytes of K and of V), a warp 8 rows of 128 channels or 16 of 64: what a
+// group needs once - range, scale, centre, reciprocal - is computed once.  A word of the V codes holds four tokens, so lanes of
+// four neighbouring rows exchange theirs and store whole words where their slots are one word's, else single bytes; rows are
+// taken so that they are: fours end where slot mod 4 is 3, judged by the sequence's first slot.  With one or two rows per sequence (decoded
+// tokens) a warp's rows are heads instead.  Bound: instructions first (8 per channel for the codes), then bytes.
+//
+// Load: 16 lanes hold a row of 128 channels (8 of 64) as 16-byte vectors.  Bound: bytes, four fifths of them written.
 constexpr int kRowThreads = 256;
 
 struct RowParams {
@@ -255,8 +257,9 @@ struct RowParams {
   uint8_t* dst[2];         // load: k_out, v_out
   uint8_t* pool;
   int32_t* workspace;
-  int32_t n_heads, rows, groups, lg;
+  int32_t n_heads, rows, groups, lg;   // groups: store: warps' shares of the rows (TOKENS: of the heads); load: fours of rows
   uint32_t n_slots;        // n_pages * page
+  uint32_t warps;          // n_heads (TOKENS: rows) * groups
   int64_t stride[2][3];    // bytes: sequence, head, row
 };
 
@@ -269,9 +272,9 @@ __device__ __forceinline__ uint8_t* chunk_of(const RowParams& p, int32_t slot, i
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 __device__ __forceinline__ uint32_t to_bf16(float x) {   // round to nearest even; NaN stays NaN
-  uint16_t h;
-  asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(x));
-  return h;
+  uint32_t w;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(0.0f), "f"(x));   // (the pair's conversion runs at four times the rate of one)
+  return w;
 }
 
 __device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {   // a NaN stays one
@@ -286,150 +289,155 @@ __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ bool finite_bf16(uint32_t bits) { return (bits & 0x7f80u) != 0x7f80u; }
 
-// Codes of eight channels as nibbles 0..7 of a word; scale and centre (bf16 bits) of the group of four lanes.
+// Codes of a group's 32 channels as nibbles 0..7 of four words; its scale and centre (bf16 bits).
 //
 // A code is round((x - z) / s) + 8, ties to even.  With d = x - z (fp32) and the reciprocal of s in two fp32 terms, q = d hi +
-// d lo is d / s to 2^-47 before its one rounding.  That decides as the correctly rounded quotient does: a tie s (k + 1/2) has 13
+// d lo is d / s to 2^-45 before its one rounding.  That decides as the correctly rounded quotient does: a tie s (k + 1/2) has 13
 // bits, so another fp32 number d is more than 2^-24 of it away, which q's rounding keeps on its side; a tie itself is kept exactly.
 // (|d / s| stays below 32: where the centre's rounding is many steps, so is the spacing of bf16 numbers beside it.)  No division
 // and no conversion per channel: both run at a quarter of the rate of what is used here (the 32 x 192 x 32 rows of a pruned prompt: 71
 // us with them, STORED without).
-__device__ __forceinline__ uint32_t quantise8(const uint4& v, uint32_t* scale, uint32_t* centre) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t lo2 = min_bf16x2(min_bf16x2(w[0], w[1]), min_bf16x2(w[2], w[3]));
-  uint32_t hi2 = max_bf16x2(max_bf16x2(w[0], w[1]), max_bf16x2(w[2], w[3]));
+__device__ __forceinline__ void quantise(const uint4 (&v)[4], uint32_t (&codes)[4], uint32_t* scale, uint32_t* centre) {
+  uint32_t lo2 = v[0].x, hi2 = v[0].x;
 #pragma unroll
-  for (int d = 1; d < 4; d <<= 1) {
-    lo2 = min_bf16x2(lo2, __shfl_xor_sync(~0u, lo2, d));
-    hi2 = max_bf16x2(hi2, __shfl_xor_sync(~0u, hi2, d));
+  for (int i = 0; i < 4; ++i) {
+    lo2 = min_bf16x2(lo2, min_bf16x2(min_bf16x2(v[i].x, v[i].y), min_bf16x2(v[i].z, v[i].w)));
+    hi2 = max_bf16x2(hi2, max_bf16x2(max_bf16x2(v[i].x, v[i].y), max_bf16x2(v[i].z, v[i].w)));
   }
   lo2 = min_bf16x2(lo2, lo2 >> 16 | lo2 << 16);
   hi2 = max_bf16x2(hi2, hi2 >> 16 | hi2 << 16);
-  if (!finite_bf16(lo2) || !finite_bf16(hi2)) {   // (the centre stays finite: the attention multiplies it by zero for hidden keys)
-    *scale = 0x7fc0u;
-    *centre = 0;
-    return 0;
-  }
-  const float lo = bf16_lo(lo2), hi = bf16_lo(hi2);
-  *scale = to_bf16(__fdiv_rn(__fsub_rn(0.5f * hi, 0.5f * lo), 7.5f));   // (halves: the difference of two finite numbers may not be one)
+  // scale: (halves: the difference of two finite numbers may not be one) over 7.5, as below
+  const float lo = bf16_lo(lo2), half = __fsub_rn(0.5f * bf16_lo(hi2), 0.5f * lo);
+  constexpr float kInv = static_cast<float>(1.0 / 7.5), kInvLow = static_cast<float>(1.0 / 7.5 - static_cast<double>(kInv));
+  *scale = to_bf16(__fmaf_rn(half, kInv, __fmul_rn(half, kInvLow)));
   const float s = __uint_as_float(*scale << 16);
   *centre = to_bf16(__fmaf_rn(8.0f, s, lo));
   const float z = __uint_as_float(*centre << 16);
-  if (s == 0.0f) return 0x88888888u;
-  if (s < 0x1p-100f) {   // a reciprocal whose second term would not be a normal number
-    uint32_t codes = 0;
-#pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-      const float x = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
-      const float c = rintf(__fdiv_rn(__fsub_rn(x, z), s)) + 8.0f;
-      codes |= static_cast<uint32_t>(fminf(fmaxf(c, 0.0f), 15.0f)) << (4 * i);
-    }
-    return codes;
-  }
-  const float hi_inv = __frcp_rn(s), lo_inv = __fmul_rn(__fmaf_rn(-s, hi_inv, 1.0f), hi_inv);
-  constexpr float kMagic = 12582912.0f;     // 1.5 x 2^23: adding it rounds to a whole number, and its bits plus that number are the sum's
-  uint32_t codes = 0;
+  if (!(s >= 0x1p-100f) || !finite_bf16(lo2) || !finite_bf16(hi2)) {
+    const bool none = !finite_bf16(lo2) || !finite_bf16(hi2);   // (the centre stays finite: the attention multiplies it by zero for hidden keys)
+    if (none) { *scale = 0x7fc0u; *centre = 0; }
 #pragma unroll
-  for (int i = 7; i >= 0; --i) {
-    const float x = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
-    const float d = __fsub_rn(x, z);
-    const float t = __fadd_rn(__fmaf_rn(d, hi_inv, __fmul_rn(d, lo_inv)), kMagic);
-    codes = codes * 16u + __float_as_uint(fminf(fmaxf(t, kMagic - 8.0f), kMagic + 7.0f));
+    for (int i = 0; i < 4; ++i) codes[i] = none ? 0u : 0x88888888u;
+    if (none || s == 0.0f) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                   // a scale whose reciprocal has no normal second term
+      const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+      uint32_t c8 = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float c = rintf(__fdiv_rn(__fsub_rn((j & 1) ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]), z), s)) + 8.0f;
+        c8 |= static_cast<uint32_t>(fminf(fmaxf(c, 0.0f), 15.0f)) << (4 * j);
+      }
+      codes[i] = c8;
+    }
+    return;
   }
-  // sum of 16^i (bits of kMagic + c_i - 8), c_i wanted
-  return codes - 0x11111111u * (0x4b400000u - 8u);
-}
-
-template <int D>
-__global__ void __launch_bounds__(kRowThreads) page_store_kernel(RowParams p) {
-  constexpr int kLanes = D / 8;              // lanes of a row
-  constexpr int kPer = 4 * kLanes / 32;      // rows of a lane: 2, or 1 with 64 channels
-  using C = Chunk<D>;
-  pdl_launch_dependents();
-  pdl_wait();
-  const int seq = blockIdx.y, lane = threadIdx.x & 31;
-  const int64_t w = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5);
-  if (w >= static_cast<int64_t>(p.n_heads) * p.groups) return;
-  const int head = static_cast<int>(w / p.groups), grp = static_cast<int>(w % p.groups);
-  const int32_t* slots = p.slots + static_cast<int64_t>(seq) * p.rows;
-  const int32_t slot0 = slots[0];
-  const int row0 = 4 * grp - (slot0 & 3);    // (negative slots: any grouping will do)
-  int32_t slot[4];
+  float hi_inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(hi_inv) : "f"(s));
+  const float lo_inv = __fmul_rn(__fmaf_rn(-s, hi_inv, 1.0f), hi_inv);
+  constexpr float kMagic = 12582912.0f;     // 1.5 x 2^23: adding it rounds to a whole number, and its bits plus that number are the sum's
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int r = row0 + i;
-    slot[i] = r >= 0 && r < p.rows ? slots[r] : -1;
-    if (slot[i] >= 0 && static_cast<uint32_t>(slot[i]) >= p.n_slots) {
-      if (lane == 0) record_status(p.workspace, MUSTDROP_ERR_BAD_PAGE, seq);
-      slot[i] = -1;
+    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+    uint32_t c8 = 0;
+#pragma unroll
+    for (int j = 7; j >= 0; --j) {
+      const float d = __fsub_rn((j & 1) ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]), z);
+      const float t = __fadd_rn(__fmaf_rn(d, hi_inv, __fmul_rn(d, lo_inv)), kMagic);
+      c8 = c8 * 16u + __float_as_uint(fminf(fmaxf(t, kMagic - 8.0f), kMagic + 7.0f));
     }
+    codes[i] = c8 - 0x11111111u * (0x4b400000u - 8u);   // the sum of 16^j (bits of kMagic + c_j - 8): c_j wanted
   }
-  if ((slot[0] & slot[1] & slot[2] & slot[3]) < 0 && slot[0] < 0 && slot[1] < 0 && slot[2] < 0 && slot[3] < 0) return;
-  const int c8 = lane % kLanes, sub = lane / kLanes;   // channels 8 c8 .. + 7; rows sub, sub + 32 / kLanes, ..
-  const int g = c8 >> 2, t4 = c8 & 3;
-  uint4 x[2][kPer];
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    const int i = sub + u * (32 / kLanes);
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      x[kv][u] = make_uint4(0, 0, 0, 0);
-      if (slot[i] >= 0)
-        x[kv][u] = __ldg(reinterpret_cast<const uint4*>(p.src[kv] + seq * p.stride[kv][0] + head * p.stride[kv][1] +
-                                                        (row0 + i) * p.stride[kv][2] + c8 * 16));
-    }
-  }
-  uint32_t vcodes[kPer];
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    const int i = sub + u * (32 / kLanes);
-    uint32_t s, z, vs, vz;
-    const uint32_t kcodes = quantise8(x[0][u], &s, &z);
-    vcodes[u] = quantise8(x[1][u], &vs, &vz);
-    if (slot[i] >= 0) {
-      uint8_t* const c = chunk_of<D>(p, slot[i], head);
-      const int r = chunk_row(slot[i]);
-      *reinterpret_cast<uint32_t*>(c + C::kK + r * (D / 2) + t4 * (4 * C::kG) + g * 4) = kcodes;
-      if (t4 == 0) {
-        uint16_t* const ksz = reinterpret_cast<uint16_t*>(c + C::kKsz) + r * 2 * C::kG + g;
-        ksz[0] = static_cast<uint16_t>(s);
-        ksz[C::kG] = static_cast<uint16_t>(z);
-        reinterpret_cast<uint16_t*>(c + C::kVs)[r * C::kG + g] = static_cast<uint16_t>(vs);
-        reinterpret_cast<uint16_t*>(c + C::kVz)[g * 16 + r] = static_cast<uint16_t>(vz);
-      }
-    }
-  }
-  // V: the four bytes of a lane's codes belong to the words (i = 2 (c8 mod 4) + b / 2, e = b mod 2), b = 0..3, of its group
-  const bool whole = slot[0] >= 0 && (slot[0] & 3) == 0 && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 && slot[3] == slot[0] + 3;
-  uint32_t row_codes[4];                                 // of all four rows, for this lane's channels
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    row_codes[i] = __shfl_sync(~0u, vcodes[i / (32 / kLanes)], (i % (32 / kLanes)) * kLanes + c8);
-  const int a = g >> 1, h = g & 1;
-  auto word_at = [&](uint8_t* c, int r8, int t, int e) { return c + C::kV + (((a * 8 + r8) * 4 + t) * 4 + h * 2 + e) * 4; };
-  if (whole) {
-    uint8_t* const c = chunk_of<D>(p, slot[0], head);
-    const int t = (slot[0] & 15) >> 2;
-    for (int j = sub; j < 2; j += 32 / kLanes) {         // the rows of the word table this lane writes: 2 (c8 mod 4) + j
-      uint32_t e0 = 0, e1 = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        e0 |= ((row_codes[i] >> (16 * j)) & 0xffu) << (8 * i);
-        e1 |= ((row_codes[i] >> (16 * j + 8)) & 0xffu) << (8 * i);
-      }
-      *reinterpret_cast<uint2*>(word_at(c, 2 * t4 + j, t, 0)) = make_uint2(e0, e1);
-    }
+}
+
+// The words of four rows' code words t = 0..3 (lanes STEP apart, this one's row is `row` mod 4) that hold byte b of word
+// t = row of all of them: an exchange of words across the lanes, then of bytes within them.
+template <int STEP>
+__device__ __forceinline__ void four_rows(const uint32_t (&codes)[4], int row, uint32_t (&w)[4]) {
+  const bool b1 = row & 2, b0 = row & 1;
+  const uint32_t k0 = b1 ? codes[2] : codes[0], k1 = b1 ? codes[3] : codes[1];
+  const uint32_t r0 = __shfl_xor_sync(~0u, b1 ? codes[0] : codes[2], 2 * STEP), r1 = __shfl_xor_sync(~0u, b1 ? codes[1] : codes[3], 2 * STEP);
+  const uint32_t own = b0 ? k1 : k0, two = b0 ? r1 : r0;          // word t of this row, and of the row two away
+  const uint32_t one = __shfl_xor_sync(~0u, b0 ? k0 : k1, STEP), three = __shfl_xor_sync(~0u, b0 ? r0 : r1, STEP);
+  const uint32_t e = b0 ? one : own, o = b0 ? own : one, e2 = b0 ? three : two, o2 = b0 ? two : three;
+  const uint32_t v0 = b1 ? e2 : e, v1 = b1 ? o2 : o, v2 = b1 ? e : e2, v3 = b1 ? o : o2;
+  const uint32_t x0 = __byte_perm(v0, v1, 0x5140), x1 = __byte_perm(v0, v1, 0x7362);
+  const uint32_t y0 = __byte_perm(v2, v3, 0x5140), y1 = __byte_perm(v2, v3, 0x7362);
+  w[0] = __byte_perm(x0, y0, 0x5410); w[1] = __byte_perm(x0, y0, 0x7632);
+  w[2] = __byte_perm(x1, y1, 0x5410); w[3] = __byte_perm(x1, y1, 0x7632);
+}
+
+// TOKENS: a warp's rows are heads (one or two rows per sequence).
+template <int D, bool TOKENS>
+__global__ void __launch_bounds__(kRowThreads) page_store_kernel(RowParams p) {
+  using C = Chunk<D>;
+  constexpr int G = C::kG, kRows = 32 / G;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int seq = blockIdx.y, lane = threadIdx.x & 31, at = lane / G, g = lane % G;
+  const uint32_t w = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  if (w >= p.warps) return;
+  const uint32_t outer = w / static_cast<uint32_t>(p.groups), grp = w - outer * p.groups;
+  const int32_t* slots = p.slots + static_cast<int64_t>(seq) * p.rows;
+  int head, row;
+  if (TOKENS) {
+    row = outer;
+    head = grp * kRows + at;
   } else {
+    head = outer;
+    row = kRows * grp - (slots[0] & 3) + at;     // (a negative first slot: any four will do)
+  }
+  int32_t slot = row >= 0 && row < p.rows && head < p.n_heads ? slots[row] : -1;
+  if (slot >= 0 && static_cast<uint32_t>(slot) >= p.n_slots) {
+    record_status(p.workspace, MUSTDROP_ERR_BAD_PAGE, seq);
+    slot = -1;
+  }
+  if (__all_sync(~0u, slot < 0)) return;
+  uint4 x[2][4];
 #pragma unroll
-    for (int u = 0; u < kPer; ++u) {
-      const int i = sub + u * (32 / kLanes);
-      if (slot[i] >= 0) {
-        uint8_t* const c = chunk_of<D>(p, slot[i], head);
-        const int key = slot[i] & 15;
+  for (int kv = 0; kv < 2; ++kv) {
+    const uint4* from = reinterpret_cast<const uint4*>(p.src[kv] + seq * p.stride[kv][0] + head * p.stride[kv][1] + row * p.stride[kv][2] + g * 64);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) word_at(c, 2 * t4 + (b >> 1), key >> 2, b & 1)[key & 3] = static_cast<uint8_t>(vcodes[u] >> (8 * b));
-      }
+    for (int i = 0; i < 4; ++i) x[kv][i] = slot >= 0 ? __ldg(from + i) : make_uint4(0, 0, 0, 0);
+  }
+  uint8_t* const c = chunk_of<D>(p, max(slot, 0), TOKENS ? min(head, p.n_heads - 1) : head);
+  const int r = chunk_row(slot), key = slot & 15;
+  uint32_t codes[4], scale, centre;
+  quantise(x[0], codes, &scale, &centre);
+  if (slot >= 0) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) *reinterpret_cast<uint32_t*>(c + C::kK + r * (D / 2) + t * (4 * G) + g * 4) = codes[t];
+    uint16_t* const ksz = reinterpret_cast<uint16_t*>(c + C::kKsz) + r * 2 * G + g;
+    ksz[0] = static_cast<uint16_t>(scale);
+    ksz[G] = static_cast<uint16_t>(centre);
+  }
+  quantise(x[1], codes, &scale, &centre);
+  if (slot >= 0) {
+    reinterpret_cast<uint16_t*>(c + C::kVs)[r * G + g] = static_cast<uint16_t>(scale);
+    reinterpret_cast<uint16_t*>(c + C::kVz)[g * 16 + r] = static_cast<uint16_t>(centre);
+  }
+  // V: byte b of word t is byte (token mod 4) of the word (i = 2 t + b / 2, e = b mod 2) of its group and four tokens
+  uint8_t* const words = c + C::kV + ((g >> 1) * 32 + (key >> 2)) * 16 + (g & 1) * 8;
+  if (!TOKENS) {
+    const int32_t lead = __shfl_sync(~0u, slot, (at & ~3) * G + g);
+    const uint32_t fits = __ballot_sync(~0u, slot >= 0 && (lead & 3) == 0 && slot == lead + (at & 3));
+    uint32_t of_four = 0;                        // the lanes of this lane's four rows
+#pragma unroll
+    for (int i = 0; i < 4; ++i) of_four |= 1u << (((at & ~3) + i) * G + g);
+    uint32_t word[4];
+    four_rows<G>(codes, at, word);
+    if ((fits & of_four) == of_four) {
+      const int t = at & 3;
+      *reinterpret_cast<uint2*>(words + (2 * t) * 64) = make_uint2(word[0], word[1]);
+      *reinterpret_cast<uint2*>(words + (2 * t + 1) * 64) = make_uint2(word[2], word[3]);
+      return;
     }
+  }
+  if (slot >= 0) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) words[(2 * t + (b >> 1)) * 64 + (b & 1) * 4 + (key & 3)] = static_cast<uint8_t>(codes[t] >> (8 * b));
   }
 }
 
@@ -453,9 +461,9 @@ __global__ void __launch_bounds__(kRowThreads) page_load_kernel(RowParams p) {
   pdl_launch_dependents();
   pdl_wait();
   const int seq = blockIdx.y, lane = threadIdx.x & 31;
-  const int64_t w = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5);
-  if (w >= static_cast<int64_t>(p.n_heads) * p.groups) return;
-  const int head = static_cast<int>(w / p.groups), grp = static_cast<int>(w % p.groups);
+  const uint32_t w = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  if (w >= p.warps) return;
+  const int head = static_cast<int>(w / static_cast<uint32_t>(p.groups)), grp = static_cast<int>(w - static_cast<uint32_t>(head) * p.groups);
   const int c8 = lane % kLanes, sub = lane / kLanes;
   const int g = c8 >> 2, t4 = c8 & 3, a = g >> 1, h = g & 1;
 #pragma unroll
@@ -564,13 +572,22 @@ mustdrop_status_t mustdrop_page_store(const mustdrop_page_config_t* c, const int
   p.pool = static_cast<uint8_t*>(pool); p.workspace = static_cast<int32_t*>(workspace);
   p.n_heads = c->n_heads; p.rows = c->rows; p.lg = page_log2(c->page);
   p.n_slots = static_cast<uint32_t>(c->n_pages) << p.lg;
-  p.groups = static_cast<int32_t>((static_cast<int64_t>(c->rows) + 3 + 3) / 4);   // (the first group may begin up to three rows before the first)
-  const int64_t blocks = (static_cast<int64_t>(c->n_heads) * p.groups + kRowThreads / 32 - 1) / (kRowThreads / 32);
-  if (blocks > INT32_MAX) return MUSTDROP_ERR_UNSUPPORTED;
+  // A warp's rows are heads where a sequence has so few rows that most lanes would have none (one row, 32 heads, 240 sequences:
+  // TOK1 us against TOK2).
+  const int per_warp = 32 / (c->head_dim / kPageGroup);
+  const bool tokens = c->rows <= 2;
+  p.groups = tokens ? (c->n_heads + per_warp - 1) / per_warp
+                    : static_cast<int32_t>((static_cast<int64_t>(c->rows) + 3 + per_warp - 1) / per_warp);   // (the first may begin up to three rows before the first)
+  const int64_t warps = static_cast<int64_t>(tokens ? c->rows : c->n_heads) * p.groups, blocks = (warps + kRowThreads / 32 - 1) / (kRowThreads / 32);
+  if (warps > INT32_MAX) return MUSTDROP_ERR_UNSUPPORTED;
+  p.warps = static_cast<uint32_t>(warps);
   const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(c->n_seq));
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  return done(c->head_dim == 128 ? launch_pdl(page_store_kernel<128>, grid, dim3(kRowThreads), 0, stream, p)
-                                 : launch_pdl(page_store_kernel<64>, grid, dim3(kRowThreads), 0, stream, p));
+  if (c->head_dim == 128)
+    return done(tokens ? launch_pdl(page_store_kernel<128, true>, grid, dim3(kRowThreads), 0, stream, p)
+                       : launch_pdl(page_store_kernel<128, false>, grid, dim3(kRowThreads), 0, stream, p));
+  return done(tokens ? launch_pdl(page_store_kernel<64, true>, grid, dim3(kRowThreads), 0, stream, p)
+                     : launch_pdl(page_store_kernel<64, false>, grid, dim3(kRowThreads), 0, stream, p));
 }
 
 mustdrop_status_t mustdrop_page_load(const mustdrop_page_config_t* c, const int32_t* slots, const void* pool, void* k_out,
@@ -589,8 +606,9 @@ mustdrop_status_t mustdrop_page_load(const mustdrop_page_config_t* c, const int3
   p.n_heads = c->n_heads; p.rows = c->rows; p.lg = page_log2(c->page);
   p.n_slots = static_cast<uint32_t>(c->n_pages) << p.lg;
   p.groups = static_cast<int32_t>((static_cast<int64_t>(c->rows) + 3) / 4);
-  const int64_t blocks = (static_cast<int64_t>(c->n_heads) * p.groups + kRowThreads / 32 - 1) / (kRowThreads / 32);
-  if (blocks > INT32_MAX) return MUSTDROP_ERR_UNSUPPORTED;
+  const int64_t warps = static_cast<int64_t>(c->n_heads) * p.groups, blocks = (warps + kRowThreads / 32 - 1) / (kRowThreads / 32);
+  if (warps > INT32_MAX) return MUSTDROP_ERR_UNSUPPORTED;
+  p.warps = static_cast<uint32_t>(warps);
   const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(c->n_seq));
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   return done(c->head_dim == 128 ? launch_pdl(page_load_kernel<128>, grid, dim3(kRowThreads), 0, stream, p)
