@@ -937,7 +937,7 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   __shared__ __align__(8) uint64_t bars[kWarps][kStages];
   __shared__ int32_t warp_sum[2][kWarps];
   __shared__ int32_t part_unit[kWarps][2];      // unit of a warp's first / last partial result, -1: none
-  __shared__ int last_s[2];
+  __shared__ int join_from[2], join_parts[2];   // units this CTA joins across CTAs: the first CTA, the number of parts (0: not this CTA)
   __shared__ __align__(16) float join_s[kWarps][kPart];
   int32_t* const first = reinterpret_cast<int32_t*>(smem + Sh::kFirst);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -995,13 +995,13 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   if (carry == 0) return;
 
   // This CTA's part of the line: an equal one, except that
-  //   - where every unit can have a CTA of its own and no warp then gets more than four chunks, it has: nothing is joined across CTAs
-  //     (one request, 32 heads, 640 keys: 7.5 us against 12.3);
+  //   - where every unit can have a CTA of its own and no warp then gets eight chunks more than with equal parts, it has: nothing is
+  //     joined across CTAs (one request, 32 heads, 640 keys: 7.5 us against 12.3);
   //   - where a part is at least four times the longest unit, its ends move to the nearest unit's, for the same reason (64 requests of
   //     200 to 1800 keys: JOINED against 83 us).
   const long long total = static_cast<long long>(carry) * units_per_seq;
   const Cut cut = cut_of(total, gridDim.x);
-  const bool own_unit = static_cast<long long>(p.n_seq) * units_per_seq <= gridDim.x && longest <= 4 * kWarps;
+  const bool own_unit = static_cast<long long>(p.n_seq) * units_per_seq <= gridDim.x && longest <= cut.per + 8 * kWarps;
   const bool whole_units = own_unit || cut.per / 4 >= longest;
   auto unit_begin = [&](int unit, int* n) {
     const int seq = unit / units_per_seq;
@@ -1214,25 +1214,25 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   // the counter of a unit is its first CTA's
   if (threadIdx.x < 2) {
     const int unit = open[threadIdx.x];
-    int last = 0;
+    int parts = 0;
     if (unit >= 0) {
       int n;
       const long long b = unit_begin(unit, &n);
-      const int c0 = cut.owner(b), c1 = cut.owner(b + n - 1);
+      const int c0 = cut.owner(b);
+      parts = cut.owner(b + n - 1) - c0 + 1;
+      join_from[threadIdx.x] = c0;
       __threadfence();
-      if (atomicInc(p.joined + c0, c1 - c0) == static_cast<unsigned>(c1 - c0)) last = 1;
+      if (atomicInc(p.joined + c0, parts - 1) != static_cast<unsigned>(parts - 1)) parts = 0;
       __threadfence();
     }
-    last_s[threadIdx.x] = last;
+    join_parts[threadIdx.x] = parts;
   }
   __syncthreads();
-#pragma unroll
+#pragma unroll 1
   for (int k = 0; k < 2; ++k) {
-    if (!last_s[k]) continue;
-    const int unit = open[k];
-    int n;
-    const long long b = unit_begin(unit, &n);
-    const int c0 = cut.owner(b), parts = cut.owner(b + n - 1) - c0 + 1, rows = rows_of(unit);
+    const int parts = join_parts[k], c0 = join_from[k];
+    if (parts == 0) continue;
+    const int unit = k == 0 ? open[0] : open[1], rows = rows_of(unit);
     const int share = max(1, kWarps / rows);        // warps of a row, each joining a run of the parts
     const int run = (parts + share - 1) / share;
     for (int base = 0; base < rows; base += kWarps / share) {
