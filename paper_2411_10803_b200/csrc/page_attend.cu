@@ -280,6 +280,7 @@ struct Wide {
   // One CTA per SM: 12 warps of up to 168 registers where one column tile needs no more (more warps hide more of a warp's
   // chain copy - logits - probabilities - out), 8 of 255 for two; ~120 KB of ring.
   static constexpr int kWarps = NT == 1 ? 12 : 8;
+  static constexpr bool kEarly = false;   // the next unit's queries before this one's results: no registers for it
   static constexpr int kStages = (NT == 1 ? 2 : 3) * (128 / D);
 
   uint32_t qf[NT][G][4];                   // q as the second operand: [g][2 m + {0, 1}], odd channels over 16
@@ -290,6 +291,8 @@ struct Wide {
   float vs_mul = 1.0f;                     // 2^-E: scales of V in units of 2^E
   uint32_t vs_most = 0;                    // largest bf16 bits of a scale that need no larger E; 0: no E yet
   int32_t least = 0, len = 0;              // fewest visible keys of any column; the sequence's length
+  uint4 next_q[NT][G];
+  int32_t next_len;
 
   Consts consts;
   int lane, r, t;
@@ -299,22 +302,28 @@ struct Wide {
     consts = make_consts();
   }
 
-  __device__ __forceinline__ void fetch(const AttendParams& p, const Cursor& at) {}
-
-  __device__ __forceinline__ void begin(const AttendParams& p, const Cursor& at) {
-    len = clamp_len(p, p.len[at.seq]);
-    least = len;
+  // asks for a unit's queries and its length: channels 8 t .. + 7 of every group of row r
+  __device__ __forceinline__ void fetch(const AttendParams& p, const Cursor& at) {
+    next_len = p.len[at.seq];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int row = at.tile * kRows + nt * 8 + r;
-      uint4 w[G];
 #pragma unroll
-      for (int g = 0; g < G; ++g) w[g] = make_uint4(0, 0, 0, 0);
+      for (int g = 0; g < G; ++g) next_q[nt][g] = make_uint4(0, 0, 0, 0);
       if (row < p.rows) {
         const uint8_t* const src = q_row(p, at.seq, at.head, row) + t * 16;
 #pragma unroll
-        for (int g = 0; g < G; ++g) w[g] = __ldg(reinterpret_cast<const uint4*>(src + g * 64));
+        for (int g = 0; g < G; ++g) next_q[nt][g] = __ldg(reinterpret_cast<const uint4*>(src + g * 64));
       }
+    }
+  }
+
+  __device__ __forceinline__ void begin(const AttendParams& p, const Cursor& at) {
+    len = clamp_len(p, next_len);
+    least = len;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const uint4(&w)[G] = next_q[nt];
       float top = 0.0f;
 #pragma unroll
       for (int g = 0; g < G; ++g) {
@@ -655,6 +664,7 @@ template <int D, int R>
 struct Narrow {
   using C = Chunk<D>;
   static constexpr int kD = D, G = D / 32, kTiles = D / 16, kRows = R;
+  static constexpr bool kEarly = true;
   static constexpr int kWarps = NARROW_WARPS, kStages = NARROW_STAGES * (128 / D);
 
   uint32_t qf[G][4];            // q as the second operand, zero outside the column's group: [2 m + {0, 1}], odd channels over 16
@@ -1143,13 +1153,14 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
       const Cursor was = at;
       if (at.rest > 0) {
         next_unit(p, at, first);
-        body.fetch(p, at);
+        if (Body::kEarly) body.fetch(p, at);
       }
       const bool whole = from_start && was.chunk == first[was.seq + 1] - first[was.seq];
       if (!whole && lane == 0) part_unit[warp][from_start] = (was.seq * p.n_heads + was.head) * p.tiles + was.tile;
       // A unit that began before the warp is its first; one that it leaves unfinished is its last: then its ring is idle.
       body.end(p, was, whole, reinterpret_cast<float*>(smem + (from_start ? warp * Sh::kWarpRing : Sh::kHeads + warp * Sh::kHeadPart)));
       if (at.left == 0) break;
+      if (!Body::kEarly) body.fetch(p, at);
     }
     if (!ok) {
       // gave up: leave only when the copies in flight have landed (bounded)
