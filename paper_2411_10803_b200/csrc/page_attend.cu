@@ -1232,9 +1232,10 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
       const int c0 = cut.owner(b);
       parts = cut.owner(b + n - 1) - c0 + 1;
       join_from[threadIdx.x] = c0;
-      __threadfence();
-      if (atomicInc(p.joined + c0, parts - 1) != static_cast<unsigned>(parts - 1)) parts = 0;
-      __threadfence();
+      // (release: this CTA's part, ordered before by the barrier; acquire: the others')
+      unsigned seen;
+      asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(seen) : "l"(p.joined + c0), "r"(parts - 1) : "memory");
+      if (seen != static_cast<unsigned>(parts - 1)) parts = 0;
     }
     join_parts[threadIdx.x] = parts;
   }
@@ -1244,7 +1245,7 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
     const int parts = join_parts[k], c0 = join_from[k];
     if (parts == 0) continue;
     const int unit = k == 0 ? open[0] : open[1], rows = rows_of(unit);
-    const int share = max(1, kWarps / rows);        // warps of a row, each joining a run of the parts
+    const int share = max(1, min(kWarps / rows, (parts + 7) / 8));   // warps of a row, each joining a run of the parts
     const int run = (parts + share - 1) / share;
     for (int base = 0; base < rows; base += kWarps / share) {
       const int row = base + warp / share, mine = warp % share;

@@ -41,7 +41,8 @@ struct TableParams {
 };
 
 constexpr int kTableThreads = 512;
-constexpr int kTableSeqs = 1024;     // most sequences of a CTA
+constexpr int kTableSeqs = kTableThreads;     // most sequences of a CTA
+constexpr int kTableBatch = 8, kTableSlots = kTableBatch * kTableThreads;   // most slots of a thread, of a CTA
 
 struct Move {       // what the call does to one sequence
   int32_t cur, grow, need, back, left;   // grow: tokens gained (0 where it shrinks or is refused for its length); left: tokens it then has
@@ -94,7 +95,7 @@ __device__ __forceinline__ int2 scan_pair(int2 v, int2* warp_sums, int2* total) 
 __device__ __forceinline__ int32_t in_ring(const TableParams& p, int32_t i) { return i < p.n_pages ? i : i - p.n_pages; }
 
 __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams p) {
-  __shared__ int2 warp_sums[kTableThreads / 32];
+  __shared__ int2 warp_sums[kTableThreads / 32], sums_before[kTableThreads / 32];
   __shared__ int32_t cur_s[kTableSeqs], grow_s[kTableSeqs], first_s[kTableSeqs];   // first_s: ring offset of the first new page
   __shared__ int32_t back_s[kTableSeqs], back_at_s[kTableSeqs];                    // pages given back, and their place behind the ring's count
   __shared__ int32_t left_s[kTableSeqs];                                           // the new length
@@ -106,30 +107,39 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
   const int32_t given_head = head, given_count = count;
   const bool bad_state = head < 0 || head >= p.n_pages || count < 0 || count > p.n_pages;
   if (bad_state) head = count = 0;   // nothing is free, nothing can be given back
-  int2 before = {0, 0}, total;
-  if (first > 0) {
+  const bool lead = blockIdx.y == 0;   // of the CTAs that share a range of sequences, the one that reports
+  // this CTA's sequences (one per thread) and the sums over those before them, behind one barrier
+  int2 before = {0, 0}, total = {0, 0};
+  int32_t taken = 0;                   // largest sum of pages asked for that is granted, among this thread's sequences
+  {
+    const int i = threadIdx.x, s = first + i, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Move m = {0, 0, 0, 0, 0, false};
+    if (i < n_own) m = move_of(p, s);
 #pragma unroll 4
-    for (int s = threadIdx.x; s < first; s += kTableThreads) {
-      const Move m = move_of(p, s);
-      before.x += m.need; before.y += m.back;
+    for (int b = threadIdx.x; b < first; b += kTableThreads) {
+      const Move x = move_of(p, b);
+      before.x += x.need; before.y += x.back;
+    }
+    int2 upto = {m.need, m.back};
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int x = __shfl_up_sync(~0u, upto.x, d), y = __shfl_up_sync(~0u, upto.y, d);
+      if (lane >= d) { upto.x += x; upto.y += y; }
     }
     before.x = __reduce_add_sync(~0u, before.x);
     before.y = __reduce_add_sync(~0u, before.y);
-    if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5] = before;
+    if (lane == 31) { warp_sums[warp] = upto; sums_before[warp] = before; }
     __syncthreads();
     before = {0, 0};
 #pragma unroll
-    for (int w = 0; w < kTableThreads / 32; ++w) { before.x += warp_sums[w].x; before.y += warp_sums[w].y; }
-  }
-  int32_t taken = 0;                   // largest sum of pages asked for that is granted, among this thread's sequences
-  const bool lead = blockIdx.y == 0;   // of the CTAs that share a range of sequences, the one that reports
-  for (int base = 0; base < n_own; base += kTableThreads) {
-    const int i = base + threadIdx.x, s = first + i;
-    Move m = {0, 0, 0, 0, 0, false};
-    if (i < n_own) m = move_of(p, s);
-    int2 upto = scan_pair({m.need, m.back}, warp_sums, &total);
+    for (int w = 0; w < kTableThreads / 32; ++w) {
+      const int2 own = warp_sums[w], old = sums_before[w];
+      before.x += old.x; before.y += old.y;
+      total.x += own.x; total.y += own.y;
+      if (w < warp) { upto.x += own.x; upto.y += own.y; }
+    }
     upto.x += before.x; upto.y += before.y;
-    before.x += total.x; before.y += total.y;
+    before.x += total.x; before.y += total.y;   // now over all sequences up to the CTA's last
     if (i < n_own) {
       const bool granted = m.need == 0 || upto.x <= count;
       if (granted && m.need > 0) taken = max(taken, upto.x);
@@ -162,24 +172,41 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
   // slots, and the table entries of the pages that begin among the new tokens
   const int t0 = blockIdx.y * p.rows_per_cta, n_t = min(p.rows_per_cta, p.rows - t0);
   const int32_t mask = (1 << p.lg) - 1;
-  const int64_t items = static_cast<int64_t>(n_own) * n_t;
+  // (a thread's page ids are all asked for before the first is used: one trip to L2 for up to kTableBatch slots)
+  const int items = n_own * n_t;                 // at most kTableSlots
   int i = threadIdx.x / n_t, t = threadIdx.x % n_t;
   const int di = kTableThreads / n_t, dt = kTableThreads % n_t;
-  for (int64_t it = threadIdx.x; it < items; it += kTableThreads) {
-    const int32_t r = t0 + t;
-    int32_t slot = -1;
-    if (r < grow_s[i]) {
-      int32_t* row = p.table + static_cast<size_t>(first + i) * p.max_pages;
-      const int32_t cur = cur_s[i], pos = cur + r, e = pos >> p.lg;
-      const int32_t had = static_cast<int32_t>((static_cast<uint32_t>(cur) + mask) >> p.lg);
-      const int32_t id = e < had ? row[e] : p.ring[in_ring(p, head + first_s[i] + (e - had))];
-      if (e >= had && (pos & mask) == 0) row[e] = id;
-      if (static_cast<uint32_t>(id) < static_cast<uint32_t>(p.n_pages)) slot = (id << p.lg) | (pos & mask);
-      else record_status(p.workspace, MUSTDROP_ERR_BAD_PAGE, first + i);
+  int32_t id[kTableBatch], at[kTableBatch];      // at: the slot's place in its page, -1: no slot
+#pragma unroll
+  for (int k = 0; k < kTableBatch; ++k) {
+    id[k] = at[k] = -1;
+    if (static_cast<int>(threadIdx.x) + k * kTableThreads < items) {
+      const int32_t r = t0 + t;
+      if (r < grow_s[i]) {
+        const int32_t cur = cur_s[i], pos = cur + r, e = pos >> p.lg;
+        const int32_t had = static_cast<int32_t>((static_cast<uint32_t>(cur) + mask) >> p.lg);
+        int32_t* const entry = p.table + static_cast<size_t>(first + i) * p.max_pages + e;
+        id[k] = e < had ? *entry : p.ring[in_ring(p, head + first_s[i] + (e - had))];
+        at[k] = pos & mask;
+        if (e >= had && at[k] == 0) *entry = id[k];
+      }
+      i += di; t += dt;
+      if (t >= n_t) { t -= n_t; ++i; }
     }
-    p.slots[static_cast<size_t>(first + i) * p.rows + r] = slot;
-    i += di; t += dt;
-    if (t >= n_t) { t -= n_t; ++i; }
+  }
+  i = threadIdx.x / n_t; t = threadIdx.x % n_t;
+#pragma unroll
+  for (int k = 0; k < kTableBatch; ++k) {
+    if (static_cast<int>(threadIdx.x) + k * kTableThreads < items) {
+      int32_t slot = -1;
+      if (at[k] >= 0) {
+        if (static_cast<uint32_t>(id[k]) < static_cast<uint32_t>(p.n_pages)) slot = (id[k] << p.lg) | at[k];
+        else record_status(p.workspace, MUSTDROP_ERR_BAD_PAGE, first + i);
+      }
+      p.slots[static_cast<size_t>(first + i) * p.rows + t0 + t] = slot;
+      i += di; t += dt;
+      if (t >= n_t) { t -= n_t; ++i; }
+    }
   }
   // Lengths and state.  Every CTA has read all of them that lie before its own, so what is updated in place waits for the CTA
   // that finishes last.
@@ -546,9 +573,8 @@ mustdrop_status_t mustdrop_page_tables(const mustdrop_page_config_t* c, const in
   p.ring = ring; p.table = page_table; p.slots = slots; p.workspace = static_cast<int32_t*>(workspace);
   p.n_seq = c->n_seq; p.lg = page_log2(c->page); p.n_pages = c->n_pages; p.max_pages = c->max_pages; p.rows = c->rows;
   // About eight slots a thread: one CTA for the small calls (which then need no ticket), and CTAs that share the rows of long ones.
-  constexpr int kItems = 8 * kTableThreads;
-  p.per_cta = static_cast<int32_t>(std::min<int64_t>(std::min(c->n_seq, kTableSeqs), std::max<int64_t>(1, kItems / c->rows)));
-  p.rows_per_cta = std::min(c->rows, kItems);
+  p.per_cta = static_cast<int32_t>(std::min<int64_t>(std::min(c->n_seq, kTableSeqs), std::max<int64_t>(1, kTableSlots / c->rows)));
+  p.rows_per_cta = std::min(c->rows, kTableSlots);
   dim3 grid(static_cast<unsigned>((c->n_seq + p.per_cta - 1) / p.per_cta), static_cast<unsigned>((static_cast<int64_t>(c->rows) + p.rows_per_cta - 1) / p.rows_per_cta));
   if (grid.y > 65535) return MUSTDROP_ERR_UNSUPPORTED;
   return done(launch_pdl(page_tables_kernel, grid, dim3(kTableThreads), 0, static_cast<cudaStream_t>(cuda_stream), p));
