@@ -255,6 +255,25 @@ __device__ __forceinline__ RowSum join_row(int n, At at, int lane) {
   return s;
 }
 
+// P s goes into fp16 over a unit 2^E of its column (and, in the layout for few rows, group): mul = 2^-E, 0 where none is set.
+// A unit is set from the pair of chunks that sets the stabiliser - their largest P s, so the tokens that now count are far from both ends of
+// fp16 - and again when P s has grown by 2^13, or when the stabiliser moves: whatever set it has then faded.
+constexpr float kUnitRoom = 13.0f;
+__device__ __forceinline__ int unit_exponent(float mul) { return 127 - static_cast<int>(__float_as_uint(mul) >> 23); }
+// log2 of a bf16 scale, from its bits: too small by less than 0.09
+__device__ __forceinline__ float scale_log2(uint32_t bits) { return fmaf(static_cast<float>(bits), 1.0f / 128.0f, -127.0f); }
+// The unit for a largest P s of 2^size; `f` receives what sums over the old unit are multiplied by.
+__device__ __forceinline__ float new_unit(float mul, float size, float* f) {
+  int e = min(max(static_cast<int>(ceilf(fmaxf(size, -1000.0f))), -100), 126);
+  *f = 1.0f;
+  if (mul != 0.0f) {
+    const int old = unit_exponent(mul);
+    e = max(e, old - 90);                       // (sums stay finite)
+    *f = ex2(static_cast<float>(old - e));
+  }
+  return __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+}
+
 // Query token of a unit's row, and the row's place among the n_q * q_heads rows of its sequence in q and out.
 __device__ __forceinline__ int token_of(const AttendParams& p, int row) { return p.group == 1 ? row : static_cast<int>(__umulhi(row, p.group_magic)); }
 __device__ __forceinline__ int64_t out_row(const AttendParams& p, int row, int head) {
@@ -288,8 +307,8 @@ struct Wide {
   float cs[NT][2];                         // log2 units per unit of the scaled product, of columns 2t, 2t + 1
   float o[NT][kTiles][4], oz[NT][4];    // out (without centres) and the centres' part, rows r, r + 8 and columns 2t, 2t + 1
   float l[NT][2], m[NT][2];                // sum (of this lane's tokens), stabiliser (kNone: no key seen)
-  float vs_mul = 1.0f;                     // 2^-E: scales of V in units of 2^E
-  uint32_t vs_most = 0;                    // largest bf16 bits of a scale that need no larger E; 0: no E yet
+  float mul[NT][2];                        // 2^-E of columns 2t, 2t + 1
+  float most;                              // log2 of the P s that these columns' units have room for
   int32_t least = 0, len = 0;              // fewest visible keys of any column; the sequence's length
   uint4 next_q[NT][G];
   int32_t next_len;
@@ -382,6 +401,7 @@ struct Wide {
         cs[nt][j] = __shfl_sync(~0u, back, (2 * t + j) * 4);
         l[nt][j] = 0.0f;
         m[nt][j] = kNone;
+        mul[nt][j] = 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < kTiles; ++i)
@@ -391,9 +411,7 @@ struct Wide {
       for (int j = 0; j < 4; ++j) oz[nt][j] = 0.0f;
     }
     if (p.causal) least = max(0, len - p.n_q + 1 + token_of(p, at.tile * kRows));
-    vs_mul = 1.0f;
-    vs_most = 0;
-
+    most = INFINITY;
   }
 
   __device__ __forceinline__ void pair(const AttendParams& p, const Cursor& at, uint32_t c0, uint32_t gone) {
@@ -493,7 +511,7 @@ struct Wide {
         }
       }
     }
-    // a logit far above the stabiliser, or a scale far above its unit: move them (rare after the first chunks)
+    // a logit far above the stabiliser, or P s above its unit's room: move them (rare after the first chunks)
     float rise[2][NT][4];
     float high = -INFINITY;
     uint32_t vs_top = 0;
@@ -512,35 +530,11 @@ struct Wide {
         for (int g = 0; g < G / 2; ++g) vs_top = max_u16x2(vs_top, vsw[hf][h][g]);
     }
     vs_top = max(vs_top & 0xffffu, vs_top >> 16);
-    if (__any_sync(~0u, high > 8.0f || vs_top > vs_most)) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float top = kNone;
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
-            top = fmaxf(top, fmaxf(sacc[hf][nt][j] * cs[nt][j], sacc[hf][nt][j + 2] * cs[nt][j]));
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-          if (top > m[nt][j] + 8.0f) {
-            const float f = ex2(m[nt][j] - top);
-            m[nt][j] = top;
-            l[nt][j] *= f;
-            oz[nt][j] *= f; oz[nt][j + 2] *= f;
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i) { o[nt][i][j] *= f; o[nt][i][j + 2] *= f; }
-          }
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-              rise[hf][nt][j + 2 * h] = fmaf(sacc[hf][nt][j + 2 * h], cs[nt][j], -m[nt][j]);
-        }
+    // (the largest logit and the largest scale of this lane's tokens, be they of the same one or not; a NaN's bits are above all scales')
+    if (__any_sync(~0u, high > 8.0f || high + scale_log2(vs_top) > most || vs_top >= 0x7f80u)) {
       // A NaN for a scale: NaN in its group's channels (by way of the centres) for the columns that see the key, and the key's
       // scale is zero from here on: a column that does not see it has P = 0, and 0 x NaN would be one.
       uint32_t none = 0;               // bit (nt, j, g)
-      vs_top = 0;
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -556,8 +550,6 @@ struct Wide {
                 for (int j = 0; j < 2; ++j)
                   if (sacc[hf][nt][2 * h + j] != -INFINITY) none |= 1u << ((nt * 2 + j) * G + g);
             }
-            const uint32_t v = vsw[hf][h][g >> 1] & half;
-            vs_top = max(vs_top, (g & 1) ? v >> 16 : v);
           }
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) none |= __shfl_xor_sync(~0u, none, d);
@@ -566,21 +558,53 @@ struct Wide {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
           if (r < G && ((none >> ((nt * 2 + j) * G + r)) & 1u)) oz[nt][j] = __uint_as_float(0x7fffffffu);
+      float size[2][2];                // log2 of the largest scale of this lane's tokens
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) vs_top = max(vs_top, __shfl_xor_sync(~0u, vs_top, d));
-      if (vs_top > vs_most) {
-        const int e = min(max(static_cast<int>(vs_top >> 7) - 127, -100), 126);
-        const float mul = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-        const float f = vs_most == 0 ? 1.0f : mul / vs_mul;
-        vs_mul = mul;
-        vs_most = min(static_cast<uint32_t>(e + 127 + 6) << 7, 0x7f7fu);      // up to 64 units
+      for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int h = 0; h < 2; ++h) {
+          uint32_t v = vsw[hf][h][0];
+          if (G == 4) v = max_u16x2(v, vsw[hf][h][G / 2 - 1]);
+          size[hf][h] = scale_log2(max(v & 0xffffu, v >> 16));
+        }
+      most = INFINITY;
 #pragma unroll
-          for (int i = 0; i < kTiles; ++i)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[nt][i][j] *= f;
-      }
+        for (int j = 0; j < 2; ++j) {
+          float top = kNone;
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+            top = fmaxf(top, fmaxf(sacc[hf][nt][j] * cs[nt][j], sacc[hf][nt][j + 2] * cs[nt][j]));
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+          const bool moves = top > m[nt][j] + 8.0f;
+          if (moves) {
+            const float f = ex2(m[nt][j] - top);
+            m[nt][j] = top;
+            l[nt][j] *= f;
+            oz[nt][j] *= f; oz[nt][j + 2] *= f;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) { o[nt][i][j] *= f; o[nt][i][j + 2] *= f; }
+          }
+          float largest = -INFINITY;   // log2 of P s
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              rise[hf][nt][j + 2 * h] = fmaf(sacc[hf][nt][j + 2 * h], cs[nt][j], -m[nt][j]);
+              largest = fmaxf(largest, rise[hf][nt][j + 2 * h] + size[hf][h]);
+            }
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, d));
+          if (moves || (mul[nt][j] != 0.0f && largest > unit_exponent(mul[nt][j]) + kUnitRoom)) {
+            float f;
+            mul[nt][j] = new_unit(mul[nt][j], largest, &f);
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) { o[nt][i][j] *= f; o[nt][i][j + 2] *= f; }
+          }
+          if (mul[nt][j] != 0.0f) most = fminf(most, unit_exponent(mul[nt][j]) + kUnitRoom);
+        }
     }
     // probabilities; P and P s, turned into second operands; out
 #pragma unroll
@@ -598,7 +622,7 @@ struct Wide {
         mma_bf16(oz[nt], vz[hf][0], 0u, vz[hf][1], 0u, pz0, pz1);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float p0 = pr[2 * h] * vs_mul, p1 = pr[2 * h + 1] * vs_mul;
+          const float p0 = pr[2 * h] * mul[nt][0], p1 = pr[2 * h + 1] * mul[nt][1];
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             const float s = (g & 1) ? bf16_hi(vsw[hf][h][g >> 1]) : bf16_lo(vsw[hf][h][g >> 1]);
@@ -625,7 +649,6 @@ struct Wide {
   __device__ __forceinline__ void end(const AttendParams& p, const Cursor& at, bool whole, float* part) {
     constexpr int kPart = D + 4;
     const int64_t out_seq = static_cast<int64_t>(p.rows) * p.n_heads * D;
-    const float unit = 1.0f / vs_mul;        // 2^E
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -634,7 +657,7 @@ struct Wide {
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
         const int in_tile = nt * 8 + 2 * t + j, row = at.tile * kRows + in_tile;
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum, unit = mul[nt][j] == 0.0f ? 1.0f : 1.0f / mul[nt][j];
         uint16_t* const dst = p.out + at.seq * out_seq + out_row(p, row, at.head) * D;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -671,8 +694,7 @@ struct Narrow {
   float qs[R], qo[2];           // sums of q over this lane's group, and over its odd channels times -72, of its columns
   float cs[R], m[R], l[R], oz[R];
   float o[kTiles][4];
-  float vs_mul;
-  uint32_t vs_most;
+  float mul[R], most;           // 2^-E of this lane's columns; log2 of the P s that their units have room for
   int32_t least, len;
   uint4 next_q;
   int32_t next_len;
@@ -733,14 +755,13 @@ struct Narrow {
       qs[j] = __shfl_sync(~0u, sum, from);
       qo[j] = -72.0f * __shfl_sync(~0u, odd, from);
       cs[j] = __shfl_sync(~0u, back, from);
-      l[j] = 0.0f; m[j] = kNone; oz[j] = 0.0f;
+      l[j] = 0.0f; m[j] = kNone; oz[j] = 0.0f; mul[j] = 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
-    vs_mul = 1.0f;
-    vs_most = 0;
+    most = INFINITY;
   }
 
   __device__ __forceinline__ void pair(const AttendParams& p, const Cursor& at, uint32_t c0, uint32_t gone) {
@@ -810,7 +831,7 @@ struct Narrow {
         }
       }
     }
-    // a logit far above the stabiliser, or a scale far above its unit: move them (rare after the first chunks)
+    // a logit far above the stabiliser, or P s above its unit's room: move them (rare after the first chunks)
     float high = -INFINITY;
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf)
@@ -819,13 +840,27 @@ struct Narrow {
 #pragma unroll
         for (int j = 0; j < R; ++j) high = fmaxf(high, fmaf(s[hf][h][j], cs[j], -m[j]));
     uint32_t vs_top = max(max(vsb[0][0], vsb[0][1]), max(vsb[1][0], vsb[1][1]));
-    if (__any_sync(~0u, high > 8.0f || vs_top > vs_most)) {
+    if (__any_sync(~0u, high > 8.0f || high + scale_log2(vs_top) > most || vs_top >= 0x7f80u)) {
+      // A NaN for a scale: NaN in its group's channels (by way of the centres) for the rows that see the key, and the key's
+      // scale is zero from here on: a row that does not see it has P = 0, and 0 x NaN would be one.
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (vsb[hf][h] > 0x7f80u) {
+            vsb[hf][h] = 0;
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+              if (s[hf][h][j] != -INFINITY) oz[j] = __uint_as_float(0x7fffffffu);
+          }
+      most = INFINITY;
 #pragma unroll
       for (int j = 0; j < R; ++j) {
         float top = fmaxf(fmaxf(s[0][0][j], s[0][1][j]) * cs[j], fmaxf(s[1][0][j], s[1][1][j]) * cs[j]);
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-        if (top > m[j] + 8.0f) {
+        const bool moves = top > m[j] + 8.0f;
+        if (moves) {
           const float f = ex2(m[j] - top);
           m[j] = top;
           l[j] *= f;
@@ -833,34 +868,20 @@ struct Narrow {
 #pragma unroll
           for (int i = 0; i < kTiles; ++i) { o[i][j] *= f; o[i][j + 2] *= f; }
         }
-      }
-      // A NaN for a scale: NaN in its group's channels (by way of the centres) for the rows that see the key, and the key's
-      // scale is zero from here on: a row that does not see it has P = 0, and 0 x NaN would be one.
-      vs_top = 0;
+        float largest = -INFINITY;     // log2 of P s
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
+        for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (vsb[hf][h] > 0x7f80u) {
-            vsb[hf][h] = 0;
+          for (int h = 0; h < 2; ++h) largest = fmaxf(largest, fmaf(s[hf][h][j], cs[j], -m[j]) + scale_log2(vsb[hf][h]));
 #pragma unroll
-            for (int j = 0; j < R; ++j)
-              if (s[hf][h][j] != -INFINITY) oz[j] = __uint_as_float(0x7fffffffu);
-          }
-          vs_top = max(vs_top, vsb[hf][h]);
+        for (int d = 4; d < 32; d <<= 1) largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, d));
+        if (moves || (mul[j] != 0.0f && largest > unit_exponent(mul[j]) + kUnitRoom)) {
+          float f;
+          mul[j] = new_unit(mul[j], largest, &f);
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) { o[i][j] *= f; o[i][j + 2] *= f; }
         }
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) vs_top = max(vs_top, __shfl_xor_sync(~0u, vs_top, d));
-      if (vs_top > vs_most) {
-        const int e = min(max(static_cast<int>(vs_top >> 7) - 127, -100), 126);
-        const float mul = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-        const float f = vs_most == 0 ? 1.0f : mul / vs_mul;
-        vs_mul = mul;
-        vs_most = min(static_cast<uint32_t>(e + 127 + 6) << 7, 0x7f7fu);      // up to 64 units
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[i][j] *= f;
+        if (mul[j] != 0.0f) most = fminf(most, unit_exponent(mul[j]) + kUnitRoom);
       }
     }
 #pragma unroll
@@ -869,14 +890,14 @@ struct Narrow {
       uint32_t pv[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float vs = __uint_as_float(vsb[hf][h] << 16) * vs_mul;
+        const float vs = __uint_as_float(vsb[hf][h] << 16);
         float u[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < R; ++j) {
           const float pr = ex2(fmaf(s[hf][h][j], cs[j], -m[j]));
           l[j] += pr;
           oz[j] = fmaf(pr, vz[hf][h], oz[j]);
-          u[j] = pr * vs;
+          u[j] = pr * mul[j] * vs;
         }
         pv[h] = transpose8x8(pack_f16(u[0], u[1]));
       }
@@ -896,7 +917,6 @@ struct Narrow {
 
   __device__ __forceinline__ void end(const AttendParams& p, const Cursor& at, bool whole, float* part) {
     constexpr int kPart = D + 4;
-    const float unit = 1.0f / vs_mul;        // 2^E
     const int64_t out_seq = static_cast<int64_t>(p.rows) * p.n_heads * D;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -906,6 +926,7 @@ struct Narrow {
         sum += __shfl_xor_sync(~0u, sum, d);
         z += __shfl_xor_sync(~0u, z, d);
       }
+      const float unit = mul[j] == 0.0f ? 1.0f : 1.0f / mul[j];
       float v[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {

@@ -371,6 +371,24 @@ def test_attend_scales_of_v_that_grow_and_shrink_along_the_keys():
     c.check(queries(rng, 1, 1, 1, 128))
 
 
+@pytest.mark.parametrize("n_q", [1, 2, 5])
+@pytest.mark.parametrize("where", [0, 100, 299])
+def test_attend_a_large_value_that_nobody_attends_to_costs_no_precision(n_q, where):
+    """Keys with a scale of V 2^20 times the others' and a logit 60 below: their share is nothing, and they must not set what the
+    others are rounded to.  And the other way round: the others' share is nothing beside one key's."""
+    rng = np.random.default_rng(where + n_q)
+    n, q = 300, np.ones((1, n_q, 1, 128))
+    k, v = 0.3 * rng.standard_normal((1, 1, n, 128)), rng.standard_normal((1, 1, n, 128))
+    k[0, 0, where] = -60 / 128 ** 0.5
+    v[0, 0, where] *= 2.0 ** 20
+    c = Case(rng, [n], heads=1, k=k, v=v)
+    c.check(bf16(q), causal=False)
+    k[0, 0, where] = 30 / 128 ** 0.5
+    v[0, 0, where] *= 2.0 ** -40
+    c = Case(rng, [n], heads=1, k=k, v=v)
+    c.check(bf16(q), causal=False)
+
+
 def test_attend_keys_of_one_value_and_zero_queries():
     rng = np.random.default_rng(15)
     k, v = np.full((1, 2, 50, 128), 0.75), np.full((1, 2, 50, 128), -1.5)
