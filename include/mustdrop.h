@@ -399,7 +399,7 @@ typedef struct {
   int32_t q_heads;    /* attend: query heads, a multiple of n_heads; heads h * q_heads / n_heads .. share K / V head h */
   int32_t n_q;        /* attend: query tokens per sequence, 1..128 */
   int32_t causal;     /* attend: 1: query token t sees keys 0 .. len - n_q + t (the queries are the last n_q tokens); 0: all len keys */
-  float   scale;      /* attend: logit scale; 0 => 1/sqrt(head_dim) */
+  float   scale;      /* attend: logit scale, 0 .. 1e37; 0 => 1/sqrt(head_dim) */
   int32_t flags;      /* must be 0 */
   /* Strides in ELEMENTS (bf16); 0 => contiguous; each a multiple of 8.  Rows of head_dim elements are contiguous. */
   int64_t k_stride_s, k_stride_h, k_stride_r;   /* store: k [n_seq, n_heads, rows, head_dim] */

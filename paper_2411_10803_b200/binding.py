@@ -562,6 +562,16 @@ class PagedCache:
         if tuple(t.shape) != tuple(shape) or t.dtype != torch.bfloat16 or t.stride(-1) != 1:
             raise ValueError("%s: bf16 %s with contiguous rows expected, got %s %s" % (name, tuple(shape), t.dtype, tuple(t.shape)))
 
+    @staticmethod
+    def _strides(t, name):
+        """Strides for the library, which reads 0 as "contiguous": axes of one element have none that matters."""
+        out = []
+        for size, stride in zip(t.shape[:-1], t.stride()):
+            if size > 1 and stride == 0:
+                raise ValueError("%s: expanded axes are not supported" % name)
+            out.append(stride if size > 1 else 0)
+        return tuple(out)
+
     def extend(self, add, rows, slots=None, stream=None):
         """Every sequence gains add[s] tokens (at most `rows`; negative: gives some back) -> slots int32 [n_seq, rows]."""
         import torch
@@ -591,7 +601,7 @@ class PagedCache:
         for name, t in (("k", k), ("v", v)):
             self._want(t, (n, self.n_heads, rows, self.head_dim), name)
         self._check(None, "store", (slots, k, v))
-        ks, vs = k.stride(), v.stride()
+        ks, vs = self._strides(k, "k"), self._strides(v, "v")
         c = self._config(("store", n, rows, ks, vs), n_seq=n, rows=rows, k_stride_s=ks[0], k_stride_h=ks[1], k_stride_r=ks[2],
                          v_stride_s=vs[0], v_stride_h=vs[1], v_stride_r=vs[2], **self._base)
         with self._on():
@@ -626,7 +636,7 @@ class PagedCache:
         if not out.is_contiguous():
             raise ValueError("out: contiguous rows expected")
         self._check(None, "attend", (q, out))
-        qs = q.stride()
+        qs = self._strides(q, "q")
         c = self._config(("attend", n, n_q, qs), n_seq=n, n_q=n_q, q_stride_s=qs[0], q_stride_t=qs[1], q_stride_h=qs[2], **self._attend)
         with self._on():
             st = mustdrop_page_attend(c, q, self.pool, self.page_table[first:], self.len[first:], out, self.workspace, stream)

@@ -1333,7 +1333,7 @@ extern "C" mustdrop_status_t mustdrop_page_attend(const mustdrop_page_config_t* 
   const mustdrop_status_t st = check_page_pool(c);
   if (st != MUSTDROP_OK) return st;
   if (c->q_heads <= 0 || c->n_q <= 0 || c->max_pages <= 0 || c->causal < 0 || c->causal > 1 || c->q_heads % c->n_heads != 0 ||
-      !(c->scale >= 0.0f) || c->scale > 3.0e38f)
+      !(c->scale >= 0.0f && c->scale <= 1.0e37f))
     return MUSTDROP_ERR_INVALID_ARG;
   if (c->n_q > 128 || c->n_seq > kMaxSeqs || static_cast<int64_t>(c->max_pages) * c->page > INT32_MAX) return MUSTDROP_ERR_UNSUPPORTED;
   const int64_t rows = static_cast<int64_t>(c->q_heads / c->n_heads) * c->n_q;

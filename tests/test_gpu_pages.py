@@ -606,3 +606,85 @@ def test_the_owner_refuses_what_it_cannot_hand_on():
         md.PagedCache(n_seq=2, n_heads=2, n_pages=8, max_pages=4, page=20)
     cache.store(slots, good, good)
     assert cache.device_status() == (0, 0)
+
+
+def test_the_owner_takes_axes_of_one_element_and_refuses_expanded_ones():
+    rng = np.random.default_rng(40)
+    cache = md.PagedCache(n_seq=6, n_heads=2, n_pages=12, max_pages=2, max_q=2)
+    k = queries(rng, 6, 2, 1, 128).as_strided((6, 2, 1, 128), (256, 128, 7, 1))       # a row axis whose stride says nothing
+    slots = cache.extend(torch.ones(6, dtype=torch.int32, device="cuda"), 1)
+    cache.store(slots, k, k)
+    out = [torch.zeros((6, 2, 1, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    cache.load(slots, *out)
+    want = pages.to_bf16(pages.values(*pages.quantise(f64(k))))
+    assert np.array_equal(f64(out[0]), want) and np.array_equal(f64(out[1]), want)
+    with pytest.raises(ValueError):
+        cache.store(slots, k[:, :1].expand(6, 2, 1, 128), k)
+    with pytest.raises(ValueError):
+        cache.attend(queries(rng, 1, 1, 2, 128).expand(6, 1, 2, 128))
+    # one layer's sequences: a slice of the tables (lengths and tables then begin at any four bytes)
+    q = queries(rng, 3, 1, 2, 128)
+    got = cache.attend(q, first=3)
+    assert torch.equal(got.transpose(1, 2), out[1][3:])                               # one key each: its value
+    assert cache.device_status() == (0, 0)
+
+
+def test_the_first_calls_of_a_process_can_be_captured(tmp_path):
+    """Kernels are loaded and set up by their first call, which may happen while a graph is recorded."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2411_10803_b200 import binding as md
+cache = md.PagedCache(n_seq=2, n_heads=2, n_pages=8, max_pages=4, q_heads=2)
+one = torch.ones(2, dtype=torch.int32, device="cuda")
+slots = torch.empty((2, 1), dtype=torch.int32, device="cuda")
+k = torch.randn((2, 2, 1, 128), device="cuda").bfloat16()
+q, out, back = torch.randn((2, 1, 2, 128), device="cuda").bfloat16(), torch.zeros((2, 1, 2, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros_like(k)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    cache.extend(one, 1, slots)
+    cache.store(slots, k, k)
+    cache.load(slots, back, None)
+    cache.attend(q, out=out)
+assert cache.len.tolist() == [0, 0]
+g.replay()
+torch.cuda.synchronize()
+assert cache.len.tolist() == [1, 1] and cache.device_status() == (0, 0)
+assert torch.equal(out.transpose(1, 2), back) and back.any()
+print("fine")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
+
+
+def test_two_graphs_with_workspaces_of_their_own_replay_side_by_side():
+    rng = np.random.default_rng(41)
+    caches, graphs, outs, streams = [], [], [], [torch.cuda.Stream() for _ in range(2)]
+    lens = [rng.integers(1, 400, 20) for _ in range(2)]
+    for i in range(2):
+        cache = md.PagedCache(n_seq=20, n_heads=4, n_pages=600, max_pages=26, q_heads=4)
+        rows = int(lens[i].max())
+        k, v = queries(rng, 20, 4, rows, 128), queries(rng, 20, 4, rows, 128)
+        cache.store(cache.extend(i32(lens[i]), rows), k, v)
+        caches.append(cache)
+    qs = [queries(rng, 20, 1, 4, 128) for _ in range(2)]
+    want = [c.attend(q) for c, q in zip(caches, qs)]
+    torch.cuda.synchronize()
+    for i in range(2):
+        g, out = torch.cuda.CUDAGraph(), torch.zeros_like(qs[i])
+        with torch.cuda.graph(g):
+            for _ in range(5):
+                caches[i].attend(qs[i], out=out)
+        graphs.append(g)
+        outs.append(out)
+    for _ in range(10):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(outs[i], want[i]) and caches[i].device_status() == (0, 0)
