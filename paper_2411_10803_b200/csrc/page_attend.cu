@@ -1029,7 +1029,7 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   //   - where every unit can have a CTA of its own and no warp then gets eight chunks more than with equal parts, it has: nothing is
   //     joined across CTAs (one request, 32 heads, 640 keys: 7.5 us against 12.3);
   //   - where a part is at least four times the longest unit, its ends move to the nearest unit's, for the same reason (64 requests of
-  //     200 to 1800 keys: JOINED against 83 us).
+  //     200 to 1800 keys: 72 against 83 us).
   const long long total = static_cast<long long>(carry) * units_per_seq;
   const Cut cut = cut_of(total, gridDim.x);
   const bool own_unit = static_cast<long long>(p.n_seq) * units_per_seq <= gridDim.x && longest <= cut.per + 8 * kWarps;

@@ -32,7 +32,7 @@ namespace {
 // waits for another: each sums need and back over the sequences before its own (two loads per sequence, from L2) and
 // handles its own ones.  What the others still read - lengths and state that are updated in place - is written by the CTA that finishes
 // last; one CTA alone, or outputs of their own, need no such order.  Bound: launch and three dependent trips to L2
-// (240 sequences, one token: TAB1 us, where an empty kernel takes 2.3), the slots written for large calls.
+// (240 sequences, one token: 4.3 us), the slots written for large calls.
 struct TableParams {
   const int32_t *add, *len, *state;
   int32_t *len_out, *state_out, *ring, *table, *slots;
@@ -272,8 +272,8 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
 // Store: a lane has one row's group of 32 channels (64 bytes of K and of V), a warp 8 rows of 128 channels or 16 of 64: what a
 // group needs once - range, scale, centre, reciprocal - is computed once.  A word of the V codes holds four tokens, so lanes of
 // four neighbouring rows exchange theirs and store whole words where their slots are one word's, else single bytes; rows are
-// taken so that they are: fours end where slot mod 4 is 3, judged by the sequence's first slot.  With one or two rows per sequence (decoded
-// tokens) a warp's rows are heads instead.  Bound: instructions first (8 per channel for the codes), then bytes.
+// taken so that they are: fours end where slot mod 4 is 3, judged by the sequence's first slot.  With one row per sequence (decoded tokens) a
+// warp's rows are heads instead.  Bound: instructions first (8 per channel for the codes), then bytes.
 //
 // Load: 16 lanes hold a row of 128 channels (8 of 64) as 16-byte vectors.  Bound: bytes, four fifths of them written.
 constexpr int kRowThreads = 256;
@@ -323,7 +323,7 @@ __device__ __forceinline__ bool finite_bf16(uint32_t bits) { return (bits & 0x7f
 // bits, so another fp32 number d is more than 2^-24 of it away, which q's rounding keeps on its side; a tie itself is kept exactly.
 // (|d / s| stays below 32: where the centre's rounding is many steps, so is the spacing of bf16 numbers beside it.)  No division
 // and no conversion per channel: both run at a quarter of the rate of what is used here (the 32 x 192 x 32 rows of a pruned prompt: 71
-// us with them, STORED without).
+// us with them, 34 without).
 __device__ __forceinline__ void quantise(const uint4 (&v)[4], uint32_t (&codes)[4], uint32_t* scale, uint32_t* centre) {
   uint32_t lo2 = v[0].x, hi2 = v[0].x;
 #pragma unroll
@@ -377,24 +377,27 @@ __device__ __forceinline__ void quantise(const uint4 (&v)[4], uint32_t (&codes)[
   }
 }
 
-// The words of four rows' code words t = 0..3 (lanes STEP apart, this one's row is `row` mod 4) that hold byte b of word
-// t = row of all of them: an exchange of words across the lanes, then of bytes within them.
+// v[j] = codes[this lane's place] of the j-th of four lanes, STEP apart; `place` is this lane's (mod 4).
 template <int STEP>
-__device__ __forceinline__ void four_rows(const uint32_t (&codes)[4], int row, uint32_t (&w)[4]) {
-  const bool b1 = row & 2, b0 = row & 1;
+__device__ __forceinline__ void gather4(const uint32_t (&codes)[4], int place, uint32_t (&v)[4]) {
+  const bool b1 = place & 2, b0 = place & 1;
   const uint32_t k0 = b1 ? codes[2] : codes[0], k1 = b1 ? codes[3] : codes[1];
   const uint32_t r0 = __shfl_xor_sync(~0u, b1 ? codes[0] : codes[2], 2 * STEP), r1 = __shfl_xor_sync(~0u, b1 ? codes[1] : codes[3], 2 * STEP);
-  const uint32_t own = b0 ? k1 : k0, two = b0 ? r1 : r0;          // word t of this row, and of the row two away
+  const uint32_t own = b0 ? k1 : k0, two = b0 ? r1 : r0;          // of this lane, and of the one two places away
   const uint32_t one = __shfl_xor_sync(~0u, b0 ? k0 : k1, STEP), three = __shfl_xor_sync(~0u, b0 ? r0 : r1, STEP);
   const uint32_t e = b0 ? one : own, o = b0 ? own : one, e2 = b0 ? three : two, o2 = b0 ? two : three;
-  const uint32_t v0 = b1 ? e2 : e, v1 = b1 ? o2 : o, v2 = b1 ? e : e2, v3 = b1 ? o : o2;
-  const uint32_t x0 = __byte_perm(v0, v1, 0x5140), x1 = __byte_perm(v0, v1, 0x7362);
-  const uint32_t y0 = __byte_perm(v2, v3, 0x5140), y1 = __byte_perm(v2, v3, 0x7362);
+  v[0] = b1 ? e2 : e; v[1] = b1 ? o2 : o; v[2] = b1 ? e : e2; v[3] = b1 ? o : o2;
+}
+
+// Word b of four: byte b of each of four rows' words.
+__device__ __forceinline__ void bytes4(const uint32_t (&v)[4], uint32_t (&w)[4]) {
+  const uint32_t x0 = __byte_perm(v[0], v[1], 0x5140), x1 = __byte_perm(v[0], v[1], 0x7362);
+  const uint32_t y0 = __byte_perm(v[2], v[3], 0x5140), y1 = __byte_perm(v[2], v[3], 0x7362);
   w[0] = __byte_perm(x0, y0, 0x5410); w[1] = __byte_perm(x0, y0, 0x7632);
   w[2] = __byte_perm(x1, y1, 0x5410); w[3] = __byte_perm(x1, y1, 0x7632);
 }
 
-// TOKENS: a warp's rows are heads (one or two rows per sequence).
+// TOKENS: a warp's rows are heads (one row per sequence).
 template <int D, bool TOKENS>
 __global__ void __launch_bounds__(kRowThreads) page_store_kernel(RowParams p) {
   using C = Chunk<D>;
@@ -429,42 +432,89 @@ __global__ void __launch_bounds__(kRowThreads) page_store_kernel(RowParams p) {
   }
   uint8_t* const c = chunk_of<D>(p, max(slot, 0), TOKENS ? min(head, p.n_heads - 1) : head);
   const int r = chunk_row(slot), key = slot & 15;
-  uint32_t codes[4], scale, centre;
+  uint32_t codes[4], v[4], scale, centre;
+  // One token: the lanes of its row exchange words and scales, so that each stores 16 bytes and a sector of L2 is written once
+  // (240 sequences, 32 heads: 5.7 us against 7.8).  Many: their rows' words meet in L2 soon, and the exchange costs more.
   quantise(x[0], codes, &scale, &centre);
-  if (slot >= 0) {
+  if (!TOKENS) {
+    if (slot >= 0) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) *reinterpret_cast<uint32_t*>(c + C::kK + r * (D / 2) + t * (4 * G) + g * 4) = codes[t];
-    uint16_t* const ksz = reinterpret_cast<uint16_t*>(c + C::kKsz) + r * 2 * G + g;
-    ksz[0] = static_cast<uint16_t>(scale);
-    ksz[G] = static_cast<uint16_t>(centre);
+      for (int t = 0; t < 4; ++t) *reinterpret_cast<uint32_t*>(c + C::kK + r * (D / 2) + t * (4 * G) + g * 4) = codes[t];
+      uint16_t* const ksz = reinterpret_cast<uint16_t*>(c + C::kKsz) + r * 2 * G + g;
+      ksz[0] = static_cast<uint16_t>(scale);
+      ksz[G] = static_cast<uint16_t>(centre);
+    }
+  } else {
+    if (G == 4) {
+      gather4<1>(codes, g, v);                   // words t = g of the four groups
+    } else {
+      const uint32_t r0 = __shfl_xor_sync(~0u, g ? codes[0] : codes[2], 1), r1 = __shfl_xor_sync(~0u, g ? codes[1] : codes[3], 1);
+      v[0] = g ? r0 : codes[0]; v[1] = g ? codes[2] : r0; v[2] = g ? r1 : codes[1]; v[3] = g ? codes[3] : r1;   // words t = 2 g, 2 g + 1 of both
+    }
+    const uint32_t own = scale | centre << 16, other = __shfl_xor_sync(~0u, own, 1);
+    const uint32_t s2 = __byte_perm(own, other, 0x5410), z2 = __byte_perm(own, other, 0x7632);   // (in even lanes: of groups g, g + 1)
+    const uint32_t s4 = __shfl_down_sync(~0u, s2, 2), z4 = __shfl_down_sync(~0u, z2, 2);
+    if (slot >= 0) {
+      *reinterpret_cast<uint4*>(c + C::kK + r * (D / 2) + g * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+      if (g == 0) {
+        if (G == 4) *reinterpret_cast<uint4*>(c + C::kKsz + r * 16) = make_uint4(s2, s4, z2, z4);
+        else *reinterpret_cast<uint2*>(c + C::kKsz + r * 8) = make_uint2(s2, z2);
+      }
+    }
   }
   quantise(x[1], codes, &scale, &centre);
-  if (slot >= 0) {
-    reinterpret_cast<uint16_t*>(c + C::kVs)[r * G + g] = static_cast<uint16_t>(scale);
-    reinterpret_cast<uint16_t*>(c + C::kVz)[g * 16 + r] = static_cast<uint16_t>(centre);
-  }
-  // V: byte b of word t is byte (token mod 4) of the word (i = 2 t + b / 2, e = b mod 2) of its group and four tokens
-  uint8_t* const words = c + C::kV + ((g >> 1) * 32 + (key >> 2)) * 16 + (g & 1) * 8;
   if (!TOKENS) {
+    if (slot >= 0) reinterpret_cast<uint16_t*>(c + C::kVs)[r * G + g] = static_cast<uint16_t>(scale);
+  } else {
+    const uint32_t s2 = __byte_perm(scale, __shfl_xor_sync(~0u, scale, 1), 0x5410), s4 = __shfl_down_sync(~0u, s2, 2);
+    if (slot >= 0 && g == 0) {
+      if (G == 4) *reinterpret_cast<uint2*>(c + C::kVs + r * 8) = make_uint2(s2, s4);
+      else *reinterpret_cast<uint32_t*>(c + C::kVs + r * 4) = s2;
+    }
+  }
+  if (slot >= 0) reinterpret_cast<uint16_t*>(c + C::kVz)[g * 16 + r] = static_cast<uint16_t>(centre);
+  // V: byte b of word t is byte (token mod 4) of the word (i = 2 t + b / 2, e = b mod 2) of its group and four tokens
+  if (!TOKENS) {
+    uint8_t* const words = c + C::kV + ((g >> 1) * 32 + (key >> 2)) * 16 + (g & 1) * 8;
     const int32_t lead = __shfl_sync(~0u, slot, (at & ~3) * G + g);
     const uint32_t fits = __ballot_sync(~0u, slot >= 0 && (lead & 3) == 0 && slot == lead + (at & 3));
     uint32_t of_four = 0;                        // the lanes of this lane's four rows
 #pragma unroll
     for (int i = 0; i < 4; ++i) of_four |= 1u << (((at & ~3) + i) * G + g);
     uint32_t word[4];
-    four_rows<G>(codes, at, word);
+    gather4<G>(codes, at, v);                    // words t = at mod 4 of the four rows
+    bytes4(v, word);
     if ((fits & of_four) == of_four) {
       const int t = at & 3;
       *reinterpret_cast<uint2*>(words + (2 * t) * 64) = make_uint2(word[0], word[1]);
       *reinterpret_cast<uint2*>(words + (2 * t + 1) * 64) = make_uint2(word[2], word[3]);
-      return;
+    } else if (slot >= 0) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) words[(2 * t + (b >> 1)) * 64 + (b & 1) * 4 + (key & 3)] = static_cast<uint8_t>(codes[t] >> (8 * b));
     }
-  }
-  if (slot >= 0) {
+  } else {
+    // one token's bytes: the four of a sector from one instruction (lanes g = 2 h + e; with two groups lanes h, each both e)
+    constexpr int kPairs = G / 2;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int a = 0; a < kPairs; ++a)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) words[(2 * t + (b >> 1)) * 64 + (b & 1) * 4 + (key & 3)] = static_cast<uint8_t>(codes[t] >> (8 * b));
+      for (int t = 0; t < 4; ++t) {
+        const int h = G == 4 ? g >> 1 : g;
+        const uint32_t w = __shfl_sync(~0u, codes[t], at * G + 2 * a + h);
+        uint8_t* const to = c + C::kV + ((a * 8 + 2 * t) * 4 + (key >> 2)) * 16 + h * 8 + (key & 3);
+        if (slot >= 0) {
+          if (G == 4) {
+            const uint32_t mine = w >> (8 * (g & 1));
+            to[(g & 1) * 4] = static_cast<uint8_t>(mine);
+            to[64 + (g & 1) * 4] = static_cast<uint8_t>(mine >> 16);
+          } else {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) to[(b >> 1) * 64 + (b & 1) * 4] = static_cast<uint8_t>(w >> (8 * b));
+          }
+        }
+      }
   }
 }
 
@@ -598,10 +648,10 @@ mustdrop_status_t mustdrop_page_store(const mustdrop_page_config_t* c, const int
   p.pool = static_cast<uint8_t*>(pool); p.workspace = static_cast<int32_t*>(workspace);
   p.n_heads = c->n_heads; p.rows = c->rows; p.lg = page_log2(c->page);
   p.n_slots = static_cast<uint32_t>(c->n_pages) << p.lg;
-  // A warp's rows are heads where a sequence has so few rows that most lanes would have none (one row, 32 heads, 240 sequences:
-  // TOK1 us against TOK2).
+  // A warp's rows are heads where a sequence has one row only and most lanes would have none (32 heads, 240 sequences: 5.7 us against
+  // 9.5; two rows: 10.3 against 9.8).
   const int per_warp = 32 / (c->head_dim / kPageGroup);
-  const bool tokens = c->rows <= 2;
+  const bool tokens = c->rows == 1;
   p.groups = tokens ? (c->n_heads + per_warp - 1) / per_warp
                     : static_cast<int32_t>((static_cast<int64_t>(c->rows) + 3 + per_warp - 1) / per_warp);   // (the first may begin up to three rows before the first)
   const int64_t warps = static_cast<int64_t>(tokens ? c->rows : c->n_heads) * p.groups, blocks = (warps + kRowThreads / 32 - 1) / (kRowThreads / 32);
