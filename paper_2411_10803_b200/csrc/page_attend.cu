@@ -285,10 +285,6 @@ __device__ __forceinline__ const uint8_t* q_row(const AttendParams& p, int seq, 
   return p.q + seq * p.q_ss + tq * p.q_st + (static_cast<int64_t>(head) * p.group + (row - tq * p.group)) * p.q_sh;
 }
 
-#ifndef NARROW_WARPS
-#define NARROW_WARPS 12
-#define NARROW_STAGES 2
-#endif
 constexpr float kNone = -3.0e38f;   // stabiliser of a column that has seen no key
 
 // What a warp holds of the unit in hand, and its arithmetic, for up to 8 NT query rows: a column each.
@@ -688,7 +684,7 @@ struct Narrow {
   using C = Chunk<D>;
   static constexpr int kD = D, G = D / 32, kTiles = D / 16, kRows = R;
   static constexpr bool kEarly = true;
-  static constexpr int kWarps = NARROW_WARPS, kStages = NARROW_STAGES * (128 / D);
+  static constexpr int kWarps = 12, kStages = 2 * (128 / D);   // (16 warps of 128 registers, or three pairs in flight: no faster)
 
   uint32_t qf[G][4];            // q as the second operand, zero outside the column's group: [2 m + {0, 1}], odd channels over 16
   float qs[R], qo[2];           // sums of q over this lane's group, and over its odd channels times -72, of its columns
@@ -967,6 +963,7 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars[kWarps][kStages];
   __shared__ int32_t warp_sum[2][kWarps];
+  __shared__ long long ends_s[2];
   __shared__ int32_t part_unit[kWarps][2];      // unit of a warp's first / last partial result, -1: none
   __shared__ int join_from[2], join_parts[2];   // units this CTA joins across CTAs: the first CTA, the number of parts (0: not this CTA)
   __shared__ __align__(16) float join_s[kWarps][kPart];
@@ -1061,14 +1058,18 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
     line0 = cut.begin(blockIdx.x);
     line1 = cut.begin(blockIdx.x + 1);
     if (whole_units) {
-      auto nearest = [&](long long x) {
-        if (x == total) return x;
-        const int s = seq_of(x), n = first[s + 1] - first[s];
-        const long long base = static_cast<long long>(first[s]) * units_per_seq;
-        return base + Cut::divide(x - base + n / 2, n) * n;
-      };
-      line0 = nearest(line0);
-      line1 = nearest(line1);
+      if (warp < 2) {                            // an end each
+        long long x = warp == 0 ? line0 : line1;
+        if (x != total) {
+          const int s = seq_of(x), n = first[s + 1] - first[s];
+          const long long base = static_cast<long long>(first[s]) * units_per_seq;
+          x = base + Cut::divide(x - base + n / 2, n) * n;
+        }
+        if (lane == 0) ends_s[warp] = x;
+      }
+      __syncthreads();
+      line0 = ends_s[0];
+      line1 = ends_s[1];
     }
   }
   if (line0 == line1) return;
