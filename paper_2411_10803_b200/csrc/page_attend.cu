@@ -9,18 +9,20 @@
 // rows - the query tokens and heads that share a K / V head - as the 8 columns.  Scales meet fp32 accumulators (K) or
 // the probabilities (V).  Codes are fp16 operands (exact); q is scaled by a power of two into fp16's range (exact but for
 // members below 2^-29 of the largest); P s is rounded once, to 11 bits, with a running power of two that keeps it in fp16's
-// range whatever the scales are.  A word of eight codes costs nine instructions (five of bits, four to take the offset off); K saves
-// two of them: half of its codes go in as 64 + c, and 72 times the sum of q over their channels is taken off again, which costs
-// four bits of fp32's 24 there; over the many tokens of V's sums it would cost more.  (e4m3 operands, in which a code is a code's
-// own bits, were slower: this GPU runs that instruction as two of fp16 behind conversions.)
+// range whatever the scales are.  A word of eight codes is five instructions of bits, and four more where the offset of its operands is
+// taken off one by one; K's, and with few rows V's, are taken off the sums instead (offsets_of, take_off).  (e4m3 operands, in which a
+// code is a code's own bits, were slower: this GPU runs that instruction as two of fp16 behind conversions.)
 //
-// Bound: HBM.  A token and head is 1.25 D bytes where bf16 has 4 D, and the arithmetic must keep up with ~23 bytes per
-// clock and SM.  Every warp walks its own range of chunks (16 tokens of one head, 20 D contiguous bytes, one bulk copy each), two
-// at a time, through its own ring in shared memory, without a barrier between warps.  The chunks of all (sequence, head, row
-// tile) units form one line that is cut into equal parts, one per warp, whatever the lengths are: no host has
-// to know them.  A unit that several warps share is joined from partial results (fp32): first those of a CTA, behind its last
-// barrier, then those of the CTAs, by the CTA that finishes last.  Both add in the order of the line: the same call gives
-// the same bits.
+// Bound: HBM where the issue slots keep up: a token and head is 1.25 D bytes where bf16 has 4 D, ~23 bytes per clock and SM, and takes
+// some 250 instructions per 16 tokens with one or two query rows, 340 with up to eight.  64 requests of 200 to 1800 keys, 32 heads: 69 us,
+// 4.8 TB/s (6.3 TB/s while every SM is at work); 2 of 90 to 131 thousand keys, 8 heads of 4 query heads: 68 us, 4.1 TB/s.
+//
+// Every warp walks its own range of chunks (16 tokens of one head, 20 D contiguous bytes, one bulk copy each), two at a
+// time, through its own ring in shared memory, without a barrier between warps.  The chunks of all (sequence, head, row tile) units form one
+// line that is cut into parts, one per CTA and then one per warp, whatever the lengths are: no host has to know
+// them.  A unit that several warps share is joined from partial results (fp32): first those of a CTA, in shared memory
+// behind its last barrier, then those of the CTAs, by the CTA that finishes last.  Both add in the order of the line: the same call
+// gives the same bits.
 #include <algorithm>
 
 #include "page_internal.h"
@@ -89,6 +91,19 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
   return w;
 }
+__device__ __forceinline__ float f16_lo(uint32_t w) {
+  float x;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.f32.f16 %0, l;\n\t}" : "=f"(x) : "r"(w));
+  return x;
+}
+__device__ __forceinline__ float f16_hi(uint32_t w) {
+  float x;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.f32.f16 %0, h;\n\t}" : "=f"(x) : "r"(w));
+  return x;
+}
+// K's codes are operands with their offsets: 1024 + c for even channels, 1024 + 16 c over a q that is divided by 16 for odd ones.  What takes
+// them off again, for codes - 8: a sum over q alone.  (Costs some eight bits of the 24 that the products' sums have: 2e-5 of a logit's spread.)
+__device__ __forceinline__ float offsets_of(float even, float odd) { return fmaf(-1032.0f, even, -72.0f * odd); }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   uint32_t d;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
@@ -104,8 +119,8 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Nibbles j and j + 4 of a word as fp16 pairs of codes - 8, for j = 0..3 (K: of 1024 + 16 c for j = 1, 3).  A nibble under the bits of 1024 reads 1024 + c
-// (bits 0..3) or 1024 + 16 c (bits 4..7); both lose their offset in one exact operation.
+// Nibbles j and j + 4 of a word as fp16 pairs, for j = 0..3.  A nibble under the bits of 1024 reads 1024 + c (bits 0..3) or 1024 + 16 c
+// (bits 4..7); CODES takes either offset off, in one exact operation a pair.
 struct Consts {   // kept in registers: as literals the compiler loads them again for every word
   uint32_t low, high, magic, sixteenth, minus72;
 };
@@ -116,23 +131,19 @@ __device__ __forceinline__ uint32_t opaque(uint32_t v) {
 __device__ __forceinline__ Consts make_consts() {
   return {opaque(0x000f000fu), opaque(0x00f000f0u), opaque(0x64006400u), opaque(0x2c002c00u), opaque(0xd480d480u)};   // .., 1/16, -72
 }
-template <bool CENTRED>
+template <bool CODES>
 __device__ __forceinline__ void unpack8(const Consts& k, uint32_t w, uint32_t (&x)[4]) {
   const uint32_t w8 = w >> 8;
-  uint32_t y[4];
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[0]) : "r"(w), "r"(k.low), "r"(k.magic));
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[1]) : "r"(w), "r"(k.high), "r"(k.magic));
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[2]) : "r"(w8), "r"(k.low), "r"(k.magic));
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y[3]) : "r"(w8), "r"(k.high), "r"(k.magic));
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x[0]) : "r"(y[0]), "r"(0x64086408u));                              // 1032
-  if (CENTRED) {
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[1]) : "r"(y[1]), "r"(k.sixteenth), "r"(k.minus72));
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[3]) : "r"(y[3]), "r"(k.sixteenth), "r"(k.minus72));
-  } else {
-    x[1] = y[1];
-    x[3] = y[3];
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[0]) : "r"(w), "r"(k.low), "r"(k.magic));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[1]) : "r"(w), "r"(k.high), "r"(k.magic));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[2]) : "r"(w8), "r"(k.low), "r"(k.magic));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[3]) : "r"(w8), "r"(k.high), "r"(k.magic));
+  if (CODES) {
+    asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(x[0]) : "r"(0x64086408u));                              // 1032
+    asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(x[1]) : "r"(k.sixteenth), "r"(k.minus72));
+    asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(x[2]) : "r"(0x64086408u));
+    asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(x[3]) : "r"(k.sixteenth), "r"(k.minus72));
   }
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x[2]) : "r"(y[2]), "r"(0x64086408u));
 }
 
 // The line of chunks: sequence s has heads * tiles units of chunks(s) chunks each.
@@ -299,7 +310,7 @@ struct Wide {
   static constexpr int kStages = (NT == 1 ? 2 : 3) * (128 / D);
 
   uint32_t qf[NT][G][4];                   // q as the second operand: [g][2 m + {0, 1}], odd channels over 16
-  uint32_t qz[NT][2], qs[NT][2];           // its sums over groups, and over their odd channels times -72, in three bf16 terms
+  uint32_t qz[NT][2], qs[NT][2];           // its sums over groups, and those that take the offsets off, in three bf16 terms
   float cs[NT][2];                         // log2 units per unit of the scaled product, of columns 2t, 2t + 1
   float o[NT][kTiles][4], oz[NT][4];    // out (without centres) and the centres' part, rows r, r + 8 and columns 2t, 2t + 1
   float l[NT][2], m[NT][2];                // sum (of this lane's tokens), stabiliser (kNone: no key seen)
@@ -352,7 +363,7 @@ struct Wide {
       const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);
       const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
       const float back = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * p.scale_log2e;
-      float sums[G], odds[G];
+      float sums[G], offs[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const uint32_t ww[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
@@ -361,21 +372,22 @@ struct Wide {
         for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(ww[i]) * up; f[2 * i + 1] = bf16_hi(ww[i]) * up; }
 #pragma unroll
         for (int i = 0; i < 4; ++i) qf[nt][g][i] = (i & 1) ? pack_f16(f[i] * 0.0625f, f[i + 4] * 0.0625f) : pack_f16(f[i], f[i + 4]);
-        float odd = (f[1] + f[3]) + (f[5] + f[7]), s = odd + ((f[0] + f[2]) + (f[4] + f[6]));
+        const float odd = (f[1] + f[3]) + (f[5] + f[7]), even = (f[0] + f[2]) + (f[4] + f[6]);
+        float s = odd + even, off = offsets_of(even, odd);
         s += __shfl_xor_sync(~0u, s, 1);
         s += __shfl_xor_sync(~0u, s, 2);
-        odd += __shfl_xor_sync(~0u, odd, 1);
-        odd += __shfl_xor_sync(~0u, odd, 2);
+        off += __shfl_xor_sync(~0u, off, 1);
+        off += __shfl_xor_sync(~0u, off, 2);
         sums[g] = s;
-        odds[g] = -72.0f * odd;
+        offs[g] = off;
       }
       // terms of the sums: operand slots 4 term + g (two groups: 2 term + g); lane t holds slots 2t, 2t + 1 and 2t + 8, 2t + 9.
       // (A q that holds an infinity or a NaN has one in its sums: its logits are none either.)
       const bool high = (G == 4) && (t & 1);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        float a = k == 0 ? (high ? sums[G - 2] : sums[0]) : (high ? odds[G - 2] : odds[0]);
-        float b = k == 0 ? (high ? sums[G - 1] : sums[1]) : (high ? odds[G - 1] : odds[1]);
+        float a = k == 0 ? (high ? sums[G - 2] : sums[0]) : (high ? offs[G - 2] : offs[0]);
+        float b = k == 0 ? (high ? sums[G - 1] : sums[1]) : (high ? offs[G - 1] : offs[1]);
         uint32_t term[3];
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
@@ -687,9 +699,11 @@ struct Narrow {
   static constexpr int kWarps = 12, kStages = 2 * (128 / D);   // (16 warps of 128 registers, or three pairs in flight: no faster)
 
   uint32_t qf[G][4];            // q as the second operand, zero outside the column's group: [2 m + {0, 1}], odd channels over 16
-  float qs[R], qo[2];           // sums of q over this lane's group, and over its odd channels times -72, of its columns
+  float qs[R], qo[2];           // sums of q over this lane's group, and those that take the offsets off, of its columns
   float cs[R], m[R], l[R], oz[R];
   float o[kTiles][4];
+  float taken[R];               // sum of P s, as rounded, that the offsets of V's codes have been added with
+  int pairs;                    // since they came off
   float mul[R], most;           // 2^-E of this lane's columns; log2 of the P s that their units have room for
   int32_t least, len;
   uint4 next_q;
@@ -731,11 +745,12 @@ struct Narrow {
     const float back = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * p.scale_log2e;
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] *= up;
-    float odd = (f[1] + f[3]) + (f[5] + f[7]), sum = odd + ((f[0] + f[2]) + (f[4] + f[6]));
+    const float odd = (f[1] + f[3]) + (f[5] + f[7]), even = (f[0] + f[2]) + (f[4] + f[6]);
+    float sum = odd + even, off = offsets_of(even, odd);
     sum += __shfl_xor_sync(~0u, sum, 1);
     sum += __shfl_xor_sync(~0u, sum, 2);
-    odd += __shfl_xor_sync(~0u, odd, 1);
-    odd += __shfl_xor_sync(~0u, odd, 2);
+    off += __shfl_xor_sync(~0u, off, 1);
+    off += __shfl_xor_sync(~0u, off, 2);
     const bool used = R == 2 || (n & 1) == 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -749,15 +764,36 @@ struct Narrow {
     for (int j = 0; j < R; ++j) {
       const int from = (2 * t + j) * 4;
       qs[j] = __shfl_sync(~0u, sum, from);
-      qo[j] = -72.0f * __shfl_sync(~0u, odd, from);
+      qo[j] = __shfl_sync(~0u, off, from);
       cs[j] = __shfl_sync(~0u, back, from);
-      l[j] = 0.0f; m[j] = kNone; oz[j] = 0.0f; mul[j] = 0.0f;
+      l[j] = 0.0f; m[j] = kNone; oz[j] = 0.0f; mul[j] = 0.0f; taken[j] = 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
     most = INFINITY;
+    pairs = 0;
+  }
+
+  // V's codes go into the sums with their offsets: 1024 + c (channels of rows r) and 1024 + 16 c (rows r + 8, which so hold 16 times
+  // theirs).  What the offsets have added is 1032 and 1152 times the sum of P s as it was rounded, kept beside: it comes
+  // off before anything is done with the sums, and every 16 pairs, as long as it is not much larger than they are (half a step of
+  // 1032 P s per chunk: 3e-4 of what 512 tokens add up to, and where all of them count alike).  Four instructions a chunk instead of 32.
+  __device__ __forceinline__ void take_off() {
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      float sum = taken[j];
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
+      taken[j] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        o[i][j] = fmaf(-1032.0f, sum, o[i][j]);
+        o[i][j + 2] = fmaf(-1152.0f, sum, o[i][j + 2]);
+      }
+    }
+    pairs = 0;
   }
 
   __device__ __forceinline__ void pair(const AttendParams& p, const Cursor& at, uint32_t c0, uint32_t gone) {
@@ -849,6 +885,7 @@ struct Narrow {
             for (int j = 0; j < R; ++j)
               if (s[hf][h][j] != -INFINITY) oz[j] = __uint_as_float(0x7fffffffu);
           }
+      take_off();
       most = INFINITY;
 #pragma unroll
       for (int j = 0; j < R; ++j) {
@@ -895,7 +932,10 @@ struct Narrow {
           oz[j] = fmaf(pr, vz[hf][h], oz[j]);
           u[j] = pr * mul[j] * vs;
         }
-        pv[h] = transpose8x8(pack_f16(u[0], u[1]));
+        const uint32_t both = pack_f16(u[0], u[1]);
+#pragma unroll
+        for (int j = 0; j < R; ++j) taken[j] += j == 0 ? f16_lo(both) : f16_hi(both);
+        pv[h] = transpose8x8(both);
       }
 #pragma unroll
       for (int a = 0; a < kTiles / 4; ++a) {
@@ -904,15 +944,17 @@ struct Narrow {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t u[4];
-          unpack8<true>(consts, ww[i], u);
+          unpack8<false>(consts, ww[i], u);
           mma_f16(o[4 * a + i], u[0], u[1], u[2], u[3], pv[0], pv[1]);
         }
       }
     }
+    if (++pairs == 16) take_off();
   }
 
   __device__ __forceinline__ void end(const AttendParams& p, const Cursor& at, bool whole, float* part) {
     constexpr int kPart = D + 4;
+    take_off();
     const int64_t out_seq = static_cast<int64_t>(p.rows) * p.n_heads * D;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -929,7 +971,7 @@ struct Narrow {
         v[i] = o[i >> 1][j + 2 * (i & 1)];
 #pragma unroll
         for (int g = 1; g < G; ++g) v[i] = pick(t == g, o[2 * g + (i >> 1)][j + 2 * (i & 1)], v[i]);
-        v[i] = fmaf(v[i], unit, z);
+        v[i] = fmaf(v[i], (i & 1) ? unit * 0.0625f : unit, z);
       }
       const int d0 = 32 * t + 4 * r;
       if (whole) {
