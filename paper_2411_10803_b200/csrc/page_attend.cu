@@ -10,8 +10,10 @@
 // the probabilities (V).  Codes are fp16 operands (exact); q is scaled by a power of two into fp16's range (exact but for
 // members below 2^-29 of the largest); P s is rounded once, to 11 bits, with a running power of two that keeps it in fp16's
 // range whatever the scales are.  A word of eight codes is five instructions of bits, and four more where the offset of its operands is
-// taken off one by one; K's, and with few rows V's, are taken off the sums instead (offsets_of, take_off).  (e4m3 operands, in which a
-// code is a code's own bits, were slower: this GPU runs that instruction as two of fp16 behind conversions.)
+// taken off one by one.  K's is taken off the sums instead (offsets_of).  Not V's: the matrix instruction's fp32 sums are cut, not
+// rounded, so an offset of 1032 P s in a sum over many tokens leaves a bias (4.5e-3 of the result, 1.6e-3 being bf16's own rounding, over
+// 1000 tokens with the offset taken off every 512).  (e4m3 operands, in which a code is a code's own bits, were slower: this GPU runs that
+// instruction as two of fp16 behind conversions.)
 //
 // Bound: HBM where the issue slots keep up: a token and head is 1.25 D bytes where bf16 has 4 D, ~23 bytes per clock and SM, and takes
 // some 250 instructions per 16 tokens with one or two query rows, 340 with up to eight.  64 requests of 200 to 1800 keys, 32 heads: 69 us,
@@ -90,16 +92,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t w;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
   return w;
-}
-__device__ __forceinline__ float f16_lo(uint32_t w) {
-  float x;
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.f32.f16 %0, l;\n\t}" : "=f"(x) : "r"(w));
-  return x;
-}
-__device__ __forceinline__ float f16_hi(uint32_t w) {
-  float x;
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.f32.f16 %0, h;\n\t}" : "=f"(x) : "r"(w));
-  return x;
 }
 // K's codes are operands with their offsets: 1024 + c for even channels, 1024 + 16 c over a q that is divided by 16 for odd ones.  What takes
 // them off again, for codes - 8: a sum over q alone.  (Costs some eight bits of the 24 that the products' sums have: 2e-5 of a logit's spread.)
@@ -702,8 +694,6 @@ struct Narrow {
   float qs[R], qo[2];           // sums of q over this lane's group, and those that take the offsets off, of its columns
   float cs[R], m[R], l[R], oz[R];
   float o[kTiles][4];
-  float taken[R];               // sum of P s, as rounded, that the offsets of V's codes have been added with
-  int pairs;                    // since they came off
   float mul[R], most;           // 2^-E of this lane's columns; log2 of the P s that their units have room for
   int32_t least, len;
   uint4 next_q;
@@ -766,34 +756,13 @@ struct Narrow {
       qs[j] = __shfl_sync(~0u, sum, from);
       qo[j] = __shfl_sync(~0u, off, from);
       cs[j] = __shfl_sync(~0u, back, from);
-      l[j] = 0.0f; m[j] = kNone; oz[j] = 0.0f; mul[j] = 0.0f; taken[j] = 0.0f;
+      l[j] = 0.0f; m[j] = kNone; oz[j] = 0.0f; mul[j] = 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
     most = INFINITY;
-    pairs = 0;
-  }
-
-  // V's codes go into the sums with their offsets: 1024 + c (channels of rows r) and 1024 + 16 c (rows r + 8, which so hold 16 times
-  // theirs).  What the offsets have added is 1032 and 1152 times the sum of P s as it was rounded, kept beside: it comes
-  // off before anything is done with the sums, and every 16 pairs, as long as it is not much larger than they are (half a step of
-  // 1032 P s per chunk: 3e-4 of what 512 tokens add up to, and where all of them count alike).  Four instructions a chunk instead of 32.
-  __device__ __forceinline__ void take_off() {
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      float sum = taken[j];
-#pragma unroll
-      for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
-      taken[j] = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        o[i][j] = fmaf(-1032.0f, sum, o[i][j]);
-        o[i][j + 2] = fmaf(-1152.0f, sum, o[i][j + 2]);
-      }
-    }
-    pairs = 0;
   }
 
   __device__ __forceinline__ void pair(const AttendParams& p, const Cursor& at, uint32_t c0, uint32_t gone) {
@@ -885,7 +854,6 @@ struct Narrow {
             for (int j = 0; j < R; ++j)
               if (s[hf][h][j] != -INFINITY) oz[j] = __uint_as_float(0x7fffffffu);
           }
-      take_off();
       most = INFINITY;
 #pragma unroll
       for (int j = 0; j < R; ++j) {
@@ -932,10 +900,7 @@ struct Narrow {
           oz[j] = fmaf(pr, vz[hf][h], oz[j]);
           u[j] = pr * mul[j] * vs;
         }
-        const uint32_t both = pack_f16(u[0], u[1]);
-#pragma unroll
-        for (int j = 0; j < R; ++j) taken[j] += j == 0 ? f16_lo(both) : f16_hi(both);
-        pv[h] = transpose8x8(both);
+        pv[h] = transpose8x8(pack_f16(u[0], u[1]));
       }
 #pragma unroll
       for (int a = 0; a < kTiles / 4; ++a) {
@@ -944,17 +909,15 @@ struct Narrow {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t u[4];
-          unpack8<false>(consts, ww[i], u);
+          unpack8<true>(consts, ww[i], u);
           mma_f16(o[4 * a + i], u[0], u[1], u[2], u[3], pv[0], pv[1]);
         }
       }
     }
-    if (++pairs == 16) take_off();
   }
 
   __device__ __forceinline__ void end(const AttendParams& p, const Cursor& at, bool whole, float* part) {
     constexpr int kPart = D + 4;
-    take_off();
     const int64_t out_seq = static_cast<int64_t>(p.rows) * p.n_heads * D;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -971,7 +934,7 @@ struct Narrow {
         v[i] = o[i >> 1][j + 2 * (i & 1)];
 #pragma unroll
         for (int g = 1; g < G; ++g) v[i] = pick(t == g, o[2 * g + (i >> 1)][j + 2 * (i & 1)], v[i]);
-        v[i] = fmaf(v[i], (i & 1) ? unit * 0.0625f : unit, z);
+        v[i] = fmaf(v[i], unit, z);
       }
       const int d0 = 32 * t + 4 * r;
       if (whole) {

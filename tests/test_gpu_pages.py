@@ -389,6 +389,40 @@ def test_attend_a_large_value_that_nobody_attends_to_costs_no_precision(n_q, whe
     c.check(bf16(q), causal=False)
 
 
+def values64(x):
+    """What stored rows stand for, float64 on the GPU (the statement of oracle/pages.py)."""
+    g = x.double().unflatten(-1, (-1, 32))
+    low, high = g.amin(-1), g.amax(-1)
+    s = ((high / 2 - low / 2) / 7.5).float().bfloat16().double()[..., None]
+    z = (low[..., None] + 8 * s).float().bfloat16().double()
+    return (z + s * (torch.round((g - z) / s) + 8).clamp(0, 15) - 8 * s).flatten(-2)
+
+
+@pytest.mark.parametrize("heads,n,L", [(2, 6, 3000), (32, 24, 1100)])
+@pytest.mark.parametrize("group,n_q", [(1, 1), (2, 1), (4, 1), (3, 4)])
+@pytest.mark.parametrize("size", [0.0, 1.0, 4.0])
+def test_attend_is_as_exact_as_its_result_type(heads, n, L, group, n_q, size):
+    """The error's norm over many rows against that of rounding the exact result to bf16, 1.15 times at most: the next terms are
+    P in bf16 times centres (a third of the values, and not all of one sign) and P s in fp16 - (1 + 0.35^2 / 2 + 2^-6)^0.5 = 1.04.
+    Sums that lose bits, or lose them to one side, show here and not in the bound of a single element; in the large case a
+    warp adds up several hundred keys of one sequence."""
+    gen = torch.Generator(device="cuda").manual_seed(heads + group)
+    rng = np.random.default_rng(heads + group)
+    d, page = 64, 64
+    k, v = (torch.randn((n, heads, L, d), device="cuda", generator=gen).bfloat16() for _ in range(2))
+    lens = i32(rng.integers(L // 3, L + 1, n))
+    cache = md.PagedCache(n_seq=n, n_heads=heads, n_pages=n * (L // page + 2), max_pages=L // page + 2, head_dim=d, page=page,
+                          q_heads=heads * group, max_q=n_q, causal=0)
+    cache.store(cache.extend(lens, L), k, v)
+    q = (torch.randn((n, n_q, heads * group, d), device="cuda", generator=gen) * size).bfloat16()
+    out = cache.attend(q)
+    z = torch.einsum("bthgd,bhjd->bhgtj", q.double().unflatten(2, (heads, group)), values64(k)) * d ** -0.5
+    z = z.masked_fill(torch.arange(L, device="cuda") >= lens[:, None, None, None, None], -np.inf)
+    want = torch.einsum("bhgtj,bhjd->bthgd", torch.softmax(z, -1), values64(v)).flatten(2, 3)
+    own, rounding = (out.double() - want).norm(), (want.bfloat16().double() - want).norm()
+    assert cache.device_status() == (0, 0) and own <= 1.15 * rounding, (own / rounding)
+
+
 def test_attend_keys_of_one_value_and_zero_queries():
     rng = np.random.default_rng(15)
     k, v = np.full((1, 2, 50, 128), 0.75), np.full((1, 2, 50, 128), -1.5)
