@@ -386,7 +386,9 @@ mustdrop_status_t mustdrop_key_set(int32_t batch, int32_t n_heads, int32_t head_
  * 4-byte aligned.  The workspace (mustdrop_page_workspace_bytes, zeroed once) starts with the status
  * word (int32 code, int32 detail); calls that may overlap on the GPU need workspaces of their own.
  * Device-detected conditions (MUSTDROP_ERR_BAD_PAGE, _BAD_LENGTH, _NO_PAGES) are recorded there and
- * never trap; detail is the sequence (mustdrop_page_attend, bad page: the id).
+ * never trap; detail is the sequence (mustdrop_page_attend, bad page: the id; mustdrop_page_tables,
+ * ring state outside its limits: -1).  A bounded wait that runs out (MUSTDROP_ERR_TIMEOUT, mustdrop_page_attend) leaves outputs
+ * unspecified, and the workspace has to be zeroed before it is used again.
  */
 typedef struct {
   int32_t n_seq;      /* sequences of the call, 1..65535 (mustdrop_page_attend: ..4096) */
@@ -394,7 +396,7 @@ typedef struct {
   int32_t head_dim;   /* 64 or 128 */
   int32_t page;       /* tokens per page: 16, 32, 64 or 128 */
   int32_t n_pages;    /* pages of the pool; n_pages * page < 2^31 */
-  int32_t max_pages;  /* entries per row of page_table; max_pages * page < 2^31 */
+  int32_t max_pages;  /* entries per row of page_table; max_pages * page < 2^31 (attend: at most 2^30), n_seq * max_pages < 2^31 */
   int32_t rows;       /* tables, store, load: rows per sequence of slots and k / v */
   int32_t q_heads;    /* attend: query heads, a multiple of n_heads; heads h * q_heads / n_heads .. share K / V head h */
   int32_t n_q;        /* attend: query tokens per sequence, 1..128 */

@@ -1080,7 +1080,8 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   if (line0 == line1) return;
   // Its warps share it by pairs of chunks.
   const int pairs = static_cast<int>((line1 - line0 + 1) / 2), n_warps = min(pairs, kWarps);
-  auto warp_begin = [&](int w) { return min(line0 + 2 * static_cast<long long>(static_cast<uint32_t>(pairs) / n_warps * w + min(w, static_cast<int>(static_cast<uint32_t>(pairs) % n_warps))), line1); };
+  const int per_warp = pairs / n_warps, more = pairs - per_warp * n_warps;
+  auto warp_begin = [&](int w) { return min(line0 + 2 * (static_cast<long long>(per_warp) * w + min(w, more)), line1); };
 
   if (warp < n_warps) {
     Cursor at;       // where the warp computes
@@ -1200,8 +1201,9 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   // ---------------------------------------------------------------- joining
   // Parts of a unit in this CTA: the last one of the warp it begins in (none, if it began before the CTA), then the first ones of
   // the warps that follow.  With few rows a warp joins the unit that begins in it, warp 0 also the one that began before the CTA; with
-  // more, or where the CTA has parts of one unit only, the warps share the rows of one unit after the other.  A unit whose parts are all here gets its output; of the others - at most the one
-  // the CTA begins in and the one it ends in - the CTA leaves one part for the CTA that comes last.
+  // more, or where the CTA has parts of one unit only, the warps share the rows of one unit after the other.  A unit whose parts are all
+  // here gets its output; of the others - at most the one the CTA begins in and the one it ends in - the CTA leaves one part for the
+  // CTA that comes last.
   __syncthreads();
   auto write_out = [&](int unit, int in_tile, const RowSum& s) {
     const int seq = unit / units_per_seq, u = unit - seq * units_per_seq;
@@ -1341,7 +1343,7 @@ extern "C" mustdrop_status_t mustdrop_page_attend(const mustdrop_page_config_t* 
   if (c->q_heads <= 0 || c->n_q <= 0 || c->max_pages <= 0 || c->causal < 0 || c->causal > 1 || c->q_heads % c->n_heads != 0 ||
       !(c->scale >= 0.0f && c->scale <= 1.0e37f))
     return MUSTDROP_ERR_INVALID_ARG;
-  if (c->n_q > 128 || c->n_seq > kMaxSeqs || static_cast<int64_t>(c->max_pages) * c->page > INT32_MAX) return MUSTDROP_ERR_UNSUPPORTED;
+  if (c->n_q > 128 || c->n_seq > kMaxSeqs || static_cast<int64_t>(c->max_pages) * c->page > (1 << 30)) return MUSTDROP_ERR_UNSUPPORTED;   // (token numbers, and a pair of chunks beyond them, in 32 bits)
   const int64_t rows = static_cast<int64_t>(c->q_heads / c->n_heads) * c->n_q;
   if (rows > 16384 || c->q_heads > 65535) return MUSTDROP_ERR_UNSUPPORTED;
   // the line of chunks: sequences' chunks add up in 32 bits, units fit a grid

@@ -126,6 +126,8 @@ def test_sizes_every_call_refuses(bad, code):
     ("attend", dict(scale=float("inf")), md.MUSTDROP_ERR_INVALID_ARG),
     ("attend", dict(q_stride_t=4), md.MUSTDROP_ERR_UNSUPPORTED), ("attend", dict(max_pages=0), md.MUSTDROP_ERR_INVALID_ARG),
     ("attend", dict(n_seq=4096, max_pages=1 << 20), md.MUSTDROP_ERR_UNSUPPORTED),
+    ("attend", dict(max_pages=(1 << 26) + 1), md.MUSTDROP_ERR_UNSUPPORTED), ("tables", dict(n_seq=65535, max_pages=1 << 16), md.MUSTDROP_ERR_UNSUPPORTED),
+    ("attend", dict(scale=1e38), md.MUSTDROP_ERR_INVALID_ARG),
 ])
 def test_sizes_one_call_refuses(name, bad, code):
     assert _call(name, md.PageConfig(**{**GOOD, **bad})) == code
