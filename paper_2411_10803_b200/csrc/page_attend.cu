@@ -1030,12 +1030,15 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   // This CTA's part of the line: an equal one, except that
   //   - where every unit can have a CTA of its own and no warp then gets eight chunks more than with equal parts, it has: nothing is
   //     joined across CTAs (one request, 32 heads, 640 keys: 7.5 us against 12.3);
-  //   - where a part is at least four times the longest unit, its ends move to the nearest unit's, for the same reason (64 requests of
-  //     200 to 1800 keys: 72 against 83 us).
+  //   - where that makes parts at most 72 chunks longer (4 us), their ends move to the nearest unit's, for the same reason: a join across
+  //     CTAs takes 3 to 5 us.  With units of one length, or few of them to a part, a part is then a whole number of the longest; with many
+  //     of different lengths it is about half a unit longer.  (64 requests of 200 to 1800 keys, 32 heads: 69.2 against 72.8 us, 9 of 2048 keys:
+  //     23.6 against 27.9, 6 of 700: 11.5 against 15.0; but 16 of 1000 to 4000: 55.5 against 49.7.)
   const long long total = static_cast<long long>(carry) * units_per_seq;
   const Cut cut = cut_of(total, gridDim.x);
   const bool own_unit = static_cast<long long>(p.n_seq) * units_per_seq <= gridDim.x && longest <= cut.per + 8 * kWarps;
-  const bool whole_units = own_unit || cut.per / 4 >= longest;
+  const int longer = static_cast<long long>(longest) * p.n_seq == carry || cut.per / 4 < longest ? (cut.per + longest - 1) / longest * longest - cut.per : carry / p.n_seq / 2;
+  const bool whole_units = own_unit || longer <= 72;
   auto unit_begin = [&](int unit, int* n) {
     const int seq = unit / units_per_seq;
     *n = first[seq + 1] - first[seq];
