@@ -275,7 +275,8 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
 // taken so that they are: fours end where slot mod 4 is 3, judged by the sequence's first slot.  With one row per sequence (decoded tokens) a
 // warp's rows are heads instead.  Bound: instructions first (8 per channel for the codes), then bytes.
 //
-// Load: 16 lanes hold a row of 128 channels (8 of 64) as 16-byte vectors.  Bound: bytes, four fifths of them written.
+// Load: 16 lanes hold a row of 128 channels (8 of 64) as 16-byte vectors.  Bound: the bytes written (32 x 608 x 32 rows: 82 us; a plain fill
+// of as many bytes runs at 3.8 TB/s and takes 84).
 constexpr int kRowThreads = 256;
 
 struct RowParams {
@@ -316,6 +317,18 @@ __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ bool finite_bf16(uint32_t bits) { return (bits & 0x7f80u) != 0x7f80u; }
 
+// (x - z) hi + (x - z) lo + magic for two numbers, each operation rounded.
+__device__ __forceinline__ float2 code_pair(float2 x, float minus_z, float hi, float lo, float magic) {
+  float2 t;
+  asm("{\n\t.reg .b64 d, z, h, l, m, p;\n\t"
+      "mov.b64 d, {%2, %3};\n\tmov.b64 z, {%4, %4};\n\tmov.b64 h, {%5, %5};\n\tmov.b64 l, {%6, %6};\n\tmov.b64 m, {%7, %7};\n\t"
+      "add.rn.f32x2 d, d, z;\n\tmul.rn.f32x2 p, d, l;\n\tfma.rn.f32x2 p, d, h, p;\n\tadd.rn.f32x2 p, p, m;\n\t"
+      "mov.b64 {%0, %1}, p;\n\t}"
+      : "=f"(t.x), "=f"(t.y)
+      : "f"(x.x), "f"(x.y), "f"(minus_z), "f"(hi), "f"(lo), "f"(magic));
+  return t;
+}
+
 // Codes of a group's 32 channels as nibbles 0..7 of four words; its scale and centre (bf16 bits).
 //
 // A code is round((x - z) / s) + 8, ties to even.  With d = x - z (fp32) and the reciprocal of s in two fp32 terms, q = d hi +
@@ -323,7 +336,7 @@ __device__ __forceinline__ bool finite_bf16(uint32_t bits) { return (bits & 0x7f
 // bits, so another fp32 number d is more than 2^-24 of it away, which q's rounding keeps on its side; a tie itself is kept exactly.
 // (|d / s| stays below 32: where the centre's rounding is many steps, so is the spacing of bf16 numbers beside it.)  No division
 // and no conversion per channel: both run at a quarter of the rate of what is used here (the 32 x 192 x 32 rows of a pruned prompt: 71
-// us with them, 34 without).
+// us with them, 34 without, 31 with two channels to an fp32 instruction).
 __device__ __forceinline__ void quantise(const uint4 (&v)[4], uint32_t (&codes)[4], uint32_t* scale, uint32_t* centre) {
   uint32_t lo2 = v[0].x, hi2 = v[0].x;
 #pragma unroll
@@ -368,10 +381,11 @@ __device__ __forceinline__ void quantise(const uint4 (&v)[4], uint32_t (&codes)[
     const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
     uint32_t c8 = 0;
 #pragma unroll
-    for (int j = 7; j >= 0; --j) {
-      const float d = __fsub_rn((j & 1) ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]), z);
-      const float t = __fadd_rn(__fmaf_rn(d, hi_inv, __fmul_rn(d, lo_inv)), kMagic);
-      c8 = c8 * 16u + __float_as_uint(fminf(fmaxf(t, kMagic - 8.0f), kMagic + 7.0f));
+    for (int j = 3; j >= 0; --j) {             // two channels an instruction
+      float2 t = make_float2(bf16_lo(w[j]), bf16_hi(w[j]));
+      t = code_pair(t, -z, hi_inv, lo_inv, kMagic);
+      c8 = c8 * 16u + __float_as_uint(fminf(fmaxf(t.y, kMagic - 8.0f), kMagic + 7.0f));
+      c8 = c8 * 16u + __float_as_uint(fminf(fmaxf(t.x, kMagic - 8.0f), kMagic + 7.0f));
     }
     codes[i] = c8 - 0x11111111u * (0x4b400000u - 8u);   // the sum of 16^j (bits of kMagic + c_j - 8): c_j wanted
   }
