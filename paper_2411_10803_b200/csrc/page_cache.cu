@@ -353,14 +353,14 @@ __device__ __forceinline__ void quantise(const uint4 (&v)[4], uint32_t (&codes)[
   const float s = __uint_as_float(*scale << 16);
   *centre = to_bf16(__fmaf_rn(8.0f, s, lo));
   const float z = __uint_as_float(*centre << 16);
-  if (!(s >= 0x1p-100f) || !finite_bf16(lo2) || !finite_bf16(hi2)) {
+  if (!(s >= 0x1p-100f && s <= 0x1p100f) || !finite_bf16(lo2) || !finite_bf16(hi2)) {
     const bool none = !finite_bf16(lo2) || !finite_bf16(hi2);   // (the centre stays finite: the attention multiplies it by zero for hidden keys)
     if (none) { *scale = 0x7fc0u; *centre = 0; }
 #pragma unroll
     for (int i = 0; i < 4; ++i) codes[i] = none ? 0u : 0x88888888u;
     if (none || s == 0.0f) return;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {                   // a scale whose reciprocal has no normal second term
+    for (int i = 0; i < 4; ++i) {                   // a scale whose reciprocal is too large, or has no normal second term
       const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
       uint32_t c8 = 0;
 #pragma unroll

@@ -221,6 +221,26 @@ def test_values_at_the_ends_of_the_type():
     assert np.isnan(want[0, 0, 2, :32]).all() and np.isfinite(want[0, 0, 2, 32:]).all() and np.isfinite(want[0, 0, 1]).all()
 
 
+def test_codes_of_groups_of_every_magnitude():
+    # members that are near whole and half steps of their group's scale, which runs over the exponents of the type
+    rng = np.random.default_rng(31)
+    n, rows, d = 8, 128, 128
+    step = 2.0 ** rng.integers(-133, 124, (n, 1, rows, 4, 1)) * (1 + rng.integers(0, 128, (n, 1, rows, 4, 1)) / 128)
+    off = rng.integers(-12, 12, (n, 1, rows, 4, 1)) * step * rng.integers(0, 2, (n, 1, rows, 4, 1)) / 4
+    x = np.clip(rng.integers(0, 31, (n, 1, rows, 4, 32)) / 2 * step - 7.5 * step + off, -3.3e38, 3.3e38)
+    x[..., 5] *= 2.0 ** -18
+    t = bf16(x.reshape(n, 1, rows, d))
+    slots = np.arange(n * rows, dtype=np.int32).reshape(n, rows)
+    for first in (0, 1):                                 # many rows of a sequence; one row of each
+        s, y = (slots, t) if first == 0 else (slots.reshape(-1, 1), t.reshape(n * rows, 1, 1, d))
+        cfg = md.PageConfig(n_seq=s.shape[0], n_heads=1, head_dim=d, page=16, n_pages=n * rows // 16, rows=s.shape[1])
+        pool = torch.zeros((n * rows // 16, 1, 1, 20 * d), dtype=torch.uint8, device="cuda")
+        want = pool.cpu().numpy().copy()
+        assert md.mustdrop_page_store(cfg, i32(s), y, y, pool) == md.MUSTDROP_OK
+        pages.store(want, s, f64(y), f64(y))
+        assert np.array_equal(pool.cpu().numpy(), want)
+
+
 # ------------------------------------------------------------------ attend
 
 class Case:
