@@ -16,8 +16,8 @@
 // instruction as two of fp16 behind conversions.)
 //
 // Bound: HBM where the issue slots keep up: a token and head is 1.25 D bytes where bf16 has 4 D, ~23 bytes per clock and SM, and takes
-// some 250 instructions per 16 tokens with one or two query rows, 340 with up to eight.  64 requests of 200 to 1800 keys, 32 heads: 69 us,
-// 4.8 TB/s (6.3 TB/s while every SM is at work); 2 of 90 to 131 thousand keys, 8 heads of 4 query heads: 68 us, 4.1 TB/s.
+// some 250 instructions per 16 tokens with one or two query rows, 340 with up to eight.  64 requests of 200 to 1800 keys, 32 heads: 70 us,
+// 4.7 TB/s (6.3 TB/s while every SM is at work); 2 of 90 to 131 thousand keys, 8 heads of 4 query heads: 69 us, 4.1 TB/s.
 //
 // Every warp walks its own range of chunks (16 tokens of one head, 20 D contiguous bytes, one bulk copy each), two at a
 // time, through its own ring in shared memory, without a barrier between warps.  The chunks of all (sequence, head, row tile) units form one
@@ -982,8 +982,7 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
     asm volatile("fence.proxy.async;" ::: "memory");
   }
   if (lane < 2) part_unit[warp][lane] = -1;
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_wait();     // (and no early start of the call that follows: its CTAs would crowd onto the SMs that finish first)
 
   // chunks (per unit) of the sequences before each one: 32 bits, as the host refuses more; the line has 64
   int32_t carry = 0, longest = 0;

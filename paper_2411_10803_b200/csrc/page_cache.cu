@@ -273,11 +273,15 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
 // group needs once - range, scale, centre, reciprocal - is computed once.  A word of the V codes holds four tokens, so lanes of
 // four neighbouring rows exchange theirs and store whole words where their slots are one word's, else single bytes; rows are
 // taken so that they are: fours end where slot mod 4 is 3, judged by the sequence's first slot.  With one row per sequence (decoded tokens) a
-// warp's rows are heads instead.  Bound: instructions first (8 per channel for the codes), then bytes.
+// warp's rows are heads instead.  Bound: bytes for large calls (64 x 2048 x 8 rows, 705 MB: 123 us, 5.7 TB/s), also instructions for those of
+// 100 MB (32 x 192 x 32 one after the other: 26.5 us, 5.0 TB/s).
 //
-// Load: 16 lanes hold a row of 128 channels (8 of 64) as 16-byte vectors.  Bound: the bytes written (32 x 608 x 32 rows: 82 us; a plain fill
-// of as many bytes runs at 3.8 TB/s and takes 84).
-constexpr int kRowThreads = 256;
+// Load: 16 lanes hold a row of 128 channels (8 of 64) as 16-byte vectors.  Bound: the bytes written (32 x 608 x 32 rows: 79 us, 4.0 TB/s; a
+// plain fill of as many bytes runs at 3.8).
+// Both: small CTAs, as warps that finish hold their place until the CTA's last one has (256 threads: store 2 to 7 %, load 3 % slower).  And
+// no early start of the call that follows: its CTAs would crowd onto the few SMs that are free by then and stay there (with one after 64
+// requests' attention, tables, store and attention of the next layer take 79 us, without 71; a store and a load of one token 9.4 against 7.9).
+constexpr int kRowThreads = 128;
 
 struct RowParams {
   const int32_t* slots;
@@ -416,7 +420,6 @@ template <int D, bool TOKENS>
 __global__ void __launch_bounds__(kRowThreads) page_store_kernel(RowParams p) {
   using C = Chunk<D>;
   constexpr int G = C::kG, kRows = 32 / G;
-  pdl_launch_dependents();
   pdl_wait();
   const int seq = blockIdx.y, lane = threadIdx.x & 31, at = lane / G, g = lane % G;
   const uint32_t w = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
@@ -448,7 +451,7 @@ __global__ void __launch_bounds__(kRowThreads) page_store_kernel(RowParams p) {
   const int r = chunk_row(slot), key = slot & 15;
   uint32_t codes[4], v[4], scale, centre;
   // One token: the lanes of its row exchange words and scales, so that each stores 16 bytes and a sector of L2 is written once
-  // (240 sequences, 32 heads: 5.7 us against 7.8).  Many: their rows' words meet in L2 soon, and the exchange costs more.
+  // (240 sequences, 32 heads: 4.2 us; each its own words: 2 us more).  Many: their rows' words meet in L2 soon, and the exchange costs more.
   quantise(x[0], codes, &scale, &centre);
   if (!TOKENS) {
     if (slot >= 0) {
@@ -549,7 +552,6 @@ template <int D>
 __global__ void __launch_bounds__(kRowThreads) page_load_kernel(RowParams p) {
   constexpr int kLanes = D / 8, kPer = 4 * kLanes / 32;
   using C = Chunk<D>;
-  pdl_launch_dependents();
   pdl_wait();
   const int seq = blockIdx.y, lane = threadIdx.x & 31;
   const uint32_t w = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
@@ -662,8 +664,8 @@ mustdrop_status_t mustdrop_page_store(const mustdrop_page_config_t* c, const int
   p.pool = static_cast<uint8_t*>(pool); p.workspace = static_cast<int32_t*>(workspace);
   p.n_heads = c->n_heads; p.rows = c->rows; p.lg = page_log2(c->page);
   p.n_slots = static_cast<uint32_t>(c->n_pages) << p.lg;
-  // A warp's rows are heads where a sequence has one row only and most lanes would have none (32 heads, 240 sequences: 5.7 us against
-  // 9.5; two rows: 10.3 against 9.8).
+  // A warp's rows are heads where a sequence has one row only and most lanes would have none (32 heads, 240 sequences: 4.2 us against
+  // 8.2; two rows: the other way round).
   const int per_warp = 32 / (c->head_dim / kPageGroup);
   const bool tokens = c->rows == 1;
   p.groups = tokens ? (c->n_heads + per_warp - 1) / per_warp
