@@ -969,6 +969,7 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   __shared__ __align__(8) uint64_t bars[kWarps][kStages];
   __shared__ int32_t warp_sum[2][kWarps];
   __shared__ long long ends_s[2];
+  __shared__ int split_s[2];                    // CTAs of this CTA's unit (0: cut otherwise), and the first of them
   __shared__ int32_t part_unit[kWarps][2];      // unit of a warp's first / last partial result, -1: none
   __shared__ int join_from[2], join_parts[2];   // units this CTA joins across CTAs: the first CTA, the number of parts (0: not this CTA)
   __shared__ __align__(16) float join_s[kWarps][kPart];
@@ -1027,17 +1028,53 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   if (carry == 0) return;
 
   // This CTA's part of the line: an equal one, except that
-  //   - where every unit can have a CTA of its own and no warp then gets eight chunks more than with equal parts, it has: nothing is
+  //   - where every unit can have a CTA of its own and no warp then gets six chunks more than with equal parts, it has: nothing is
   //     joined across CTAs (one request, 32 heads, 640 keys: 7.5 us against 12.3);
+  //   - where every unit can have a whole number of CTAs and parts get at most 38 chunks longer by that (2 us), they have: a CTA then
+  //     has a part of one unit only, and joins are one instead of two in a row.  (One request, 8 heads of 4 query heads, 8192 keys: 13.3 us
+  //     against 17.7, 131072 keys: 46.1 against 48.4; one of 32 heads, 4096 keys: 12.6 against 14.7; what it cannot help pays up to 0.4 us.)  No warp gets less than a pair of chunks for it: more
+  //     parts are only more to join (2 heads of 4, 3000 keys: 11.6 us; with two pairs at least 13.1).
   //   - where that makes parts at most 72 chunks longer (4 us), their ends move to the nearest unit's, for the same reason: a join across
   //     CTAs takes 3 to 5 us.  With units of one length, or few of them to a part, a part is then a whole number of the longest; with many
   //     of different lengths it is about half a unit longer.  (64 requests of 200 to 1800 keys, 32 heads: 69.2 against 72.8 us, 9 of 2048 keys:
   //     23.6 against 27.9, 6 of 700: 11.5 against 15.0; but 16 of 1000 to 4000: 55.5 against 49.7.)
   const long long total = static_cast<long long>(carry) * units_per_seq;
   const Cut cut = cut_of(total, gridDim.x);
-  const bool own_unit = static_cast<long long>(p.n_seq) * units_per_seq <= gridDim.x && longest <= cut.per + 8 * kWarps;
+  const bool few = static_cast<long long>(p.n_seq) * units_per_seq <= gridDim.x;
+  int split = 0;                    // CTAs of the unit that this CTA has a part of; 0: one of the other cuts
+  long long line0 = 0, line1 = 0;
+  if (few && p.n_seq <= 32 && longest > cut.per + 6 * kWarps) {
+    // the shortest parts, of 32 lengths, with which that many CTAs do (lane s has sequence s; in quotients that may be one too large)
+    const uint32_t n = lane < p.n_seq ? first[lane + 1] - first[lane] : 0, least = max(cut.per, 2 * kWarps), part = least + lane + lane / 4;
+    const uint32_t inv = 0xffffffffu / part + 1;
+    auto parts_of = [](uint32_t n, uint32_t part, uint32_t inv) { return n == 0 ? 0u : max(1u, __umulhi(n + part - 1, inv)); };
+    const uint32_t longest_inv = __shfl_sync(~0u, inv, 31), longest_part = least + 38;
+    if (__reduce_add_sync(~0u, parts_of(n, longest_part, longest_inv)) * units_per_seq <= gridDim.x) {
+      uint32_t ctas = 0;
+#pragma unroll 4
+      for (int s = 0; s < p.n_seq; ++s) ctas += parts_of(__shfl_sync(~0u, n, s), part, inv);
+      const int fit = __ffs(__ballot_sync(~0u, ctas * units_per_seq <= gridDim.x)) - 1;     // (lane 31's does)
+      const uint32_t k = parts_of(n, __shfl_sync(~0u, part, fit), __shfl_sync(~0u, inv, fit));
+      uint32_t upto = k * units_per_seq;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t u = __shfl_up_sync(~0u, upto, d);
+        if (lane >= d) upto += u;
+      }
+      const int s = __popc(__ballot_sync(~0u, upto <= blockIdx.x));
+      if (s >= p.n_seq) return;
+      split = __shfl_sync(~0u, k, s);
+      const int at = blockIdx.x - (__shfl_sync(~0u, upto, s) - split * units_per_seq), unit = at / split, i = at - unit * split;
+      const int chunks = __shfl_sync(~0u, n, s);
+      const Cut of_unit = cut_of(chunks, split);
+      line0 = static_cast<long long>(first[s]) * units_per_seq + static_cast<long long>(unit) * chunks + of_unit.begin(i);
+      line1 = line0 + of_unit.per + (i < of_unit.more ? 1 : 0);
+      if (threadIdx.x == 0) { split_s[0] = split; split_s[1] = blockIdx.x - i; }
+    }
+  }
+  const bool own_unit = split == 0 && few && longest <= cut.per + 8 * kWarps;
   const int longer = static_cast<long long>(longest) * p.n_seq == carry || cut.per / 4 < longest ? (cut.per + longest - 1) / longest * longest - cut.per : carry / p.n_seq / 2;
-  const bool whole_units = own_unit || longer <= 72;
+  const bool whole_units = own_unit || (split == 0 && longer <= 72);
   auto unit_begin = [&](int unit, int* n) {
     const int seq = unit / units_per_seq;
     *n = first[seq + 1] - first[seq];
@@ -1054,8 +1091,9 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
     }
     return lo;
   };
-  long long line0, line1;
-  if (own_unit) {
+  if (split > 0) {
+    // (done)
+  } else if (own_unit) {
     if (static_cast<int>(blockIdx.x) >= p.n_seq * units_per_seq) return;
     int n;
     line0 = unit_begin(blockIdx.x, &n);
@@ -1079,6 +1117,7 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
       line1 = ends_s[1];
     }
   }
+  if (split == 0 && threadIdx.x == 0) split_s[0] = 0;
   if (line0 == line1) return;
   // Its warps share it by pairs of chunks.
   const int pairs = static_cast<int>((line1 - line0 + 1) / 2), n_warps = min(pairs, kWarps);
@@ -1260,8 +1299,8 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
     if (unit >= 0) {
       int n;
       const long long b = unit_begin(unit, &n);
-      const int c0 = cut.owner(b);
-      parts = cut.owner(b + n - 1) - c0 + 1;
+      const int k = split_s[0], c0 = k > 0 ? split_s[1] : cut.owner(b);
+      parts = k > 0 ? k : cut.owner(b + n - 1) - c0 + 1;
       join_from[threadIdx.x] = c0;
       // (release: this CTA's part, ordered before by the barrier; acquire: the others')
       unsigned seen;

@@ -350,6 +350,17 @@ def test_attend_one_long_sequence_is_split_over_the_gpu():
     c.check(queries(rng, 1, 2, 7, 128))
 
 
+@pytest.mark.parametrize("lens,heads,group,n_q,d", [
+    ([3000], 2, 4, 1, 128), ([2500], 8, 1, 1, 64), ([9000], 1, 1, 1, 128), ([1300, 0, 4100], 2, 2, 1, 128), ([0, 5, 2600, 700], 3, 8, 2, 64),
+    ([700 + 90 * i for i in range(32)], 1, 1, 1, 128), ([700 + 90 * i for i in range(33)], 1, 1, 1, 128), ([2100] * 4, 4, 3, 1, 64),
+    ([40, 6000], 1, 9, 1, 128), ([1700] * 37, 4, 1, 1, 64),
+])
+def test_attend_few_units_get_whole_numbers_of_ctas(lens, heads, group, n_q, d):
+    rng = np.random.default_rng(len(lens) * heads)
+    c = Case(rng, lens, heads=heads, d=d, page=64)
+    c.check(queries(rng, len(lens), n_q, heads * group, d))
+
+
 def test_attend_many_ragged_sequences():
     rng = np.random.default_rng(10)
     lens = rng.integers(0, 90, 700)
