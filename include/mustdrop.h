@@ -410,7 +410,8 @@ typedef struct {
 } mustdrop_page_config_t;
 
 /* Bytes of the pool / of the workspace the calls need with this configuration (0: not a valid one).  The workspace has
- * 256 bytes where n_q is 0, else also room for mustdrop_page_attend's partial results. */
+ * 256 bytes where n_q is 0, else also room for mustdrop_page_attend's partial results (0 where that call refuses head_dim,
+ * n_heads, q_heads or n_q).  One for the largest n_q serves smaller ones too. */
 size_t mustdrop_page_pool_bytes(const mustdrop_page_config_t *config /* (host) */);
 size_t mustdrop_page_workspace_bytes(const mustdrop_page_config_t *config /* (host) */);
 

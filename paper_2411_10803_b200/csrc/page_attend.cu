@@ -1366,7 +1366,6 @@ cudaError_t launch_attend(const AttendParams& p, int tile, int sms, cudaStream_t
 }  // namespace
 
 size_t page_attend_partial_bytes(const mustdrop_page_config_t* c) {
-  if (c->n_heads <= 0 || c->q_heads <= 0 || c->q_heads % c->n_heads != 0 || c->n_q > 128) return 0;
   const int64_t rows = static_cast<int64_t>(c->q_heads / c->n_heads) * c->n_q;
   const size_t part_rows = static_cast<size_t>(std::min<int64_t>(rows, tile_rows(rows)));
   const size_t bytes = static_cast<size_t>(kMaxCtas) * 2 * part_rows * (c->head_dim + 4) * sizeof(float);
@@ -1379,14 +1378,11 @@ extern "C" mustdrop_status_t mustdrop_page_attend(const mustdrop_page_config_t* 
                                                   const int32_t* page_table, const int32_t* len, void* out, void* workspace,
                                                   void* cuda_stream) {
   using namespace mustdrop;
-  const mustdrop_status_t st = check_page_pool(c);
+  const mustdrop_status_t st = check_page_queries(c);
   if (st != MUSTDROP_OK) return st;
-  if (c->q_heads <= 0 || c->n_q <= 0 || c->max_pages <= 0 || c->causal < 0 || c->causal > 1 || c->q_heads % c->n_heads != 0 ||
-      !(c->scale >= 0.0f && c->scale <= 1.0e37f))
-    return MUSTDROP_ERR_INVALID_ARG;
-  if (c->n_q > 128 || c->n_seq > kMaxSeqs || static_cast<int64_t>(c->max_pages) * c->page > (1 << 30)) return MUSTDROP_ERR_UNSUPPORTED;   // (token numbers, and a pair of chunks beyond them, in 32 bits)
+  if (c->max_pages <= 0 || c->causal < 0 || c->causal > 1 || !(c->scale >= 0.0f && c->scale <= 1.0e37f)) return MUSTDROP_ERR_INVALID_ARG;
+  if (c->n_seq > kMaxSeqs || static_cast<int64_t>(c->max_pages) * c->page > (1 << 30)) return MUSTDROP_ERR_UNSUPPORTED;   // (token numbers, and a pair of chunks beyond them, in 32 bits)
   const int64_t rows = static_cast<int64_t>(c->q_heads / c->n_heads) * c->n_q;
-  if (rows > 16384 || c->q_heads > 65535) return MUSTDROP_ERR_UNSUPPORTED;
   // the line of chunks: sequences' chunks add up in 32 bits, units fit a grid
   const int64_t most = static_cast<int64_t>(c->n_seq) * c->max_pages * (c->page / kChunkTokens);
   if (most > INT32_MAX) return MUSTDROP_ERR_UNSUPPORTED;

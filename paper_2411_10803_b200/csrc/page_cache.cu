@@ -22,6 +22,14 @@ mustdrop_status_t check_page_pool(const mustdrop_page_config_t* c) {
   return MUSTDROP_OK;
 }
 
+mustdrop_status_t check_page_queries(const mustdrop_page_config_t* c) {
+  const mustdrop_status_t st = check_page_pool(c);
+  if (st != MUSTDROP_OK) return st;
+  if (c->q_heads <= 0 || c->n_q <= 0 || c->q_heads % c->n_heads != 0) return MUSTDROP_ERR_INVALID_ARG;
+  if (c->n_q > 128 || c->q_heads > 65535 || static_cast<int64_t>(c->q_heads / c->n_heads) * c->n_q > 16384) return MUSTDROP_ERR_UNSUPPORTED;
+  return MUSTDROP_OK;
+}
+
 namespace {
 
 // ---------------------------------------------------------------------------------------- page tables
@@ -616,8 +624,9 @@ size_t mustdrop_page_pool_bytes(const mustdrop_page_config_t* c) {
 }
 
 size_t mustdrop_page_workspace_bytes(const mustdrop_page_config_t* c) {
-  if (mustdrop::check_page_sizes(c) != MUSTDROP_OK) return 0;
-  return mustdrop::kWsStatusBytes + (c->n_q > 0 ? mustdrop::page_attend_partial_bytes(c) : 0);
+  // (a size is only given where the attention would take the query rows: what it writes has to lie in it)
+  if ((c != nullptr && c->n_q != 0 ? mustdrop::check_page_queries(c) : mustdrop::check_page_sizes(c)) != MUSTDROP_OK) return 0;
+  return mustdrop::kWsStatusBytes + (c->n_q != 0 ? mustdrop::page_attend_partial_bytes(c) : 0);
 }
 
 mustdrop_status_t mustdrop_page_tables(const mustdrop_page_config_t* c, const int32_t* add, const int32_t* len,

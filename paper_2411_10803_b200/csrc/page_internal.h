@@ -26,6 +26,7 @@ inline bool misaligned(const void* p, unsigned bytes) { return (reinterpret_cast
 // The sizes every call of the family needs.
 mustdrop_status_t check_page_sizes(const mustdrop_page_config_t* c);
 mustdrop_status_t check_page_pool(const mustdrop_page_config_t* c);     // ... and the pool's
-size_t page_attend_partial_bytes(const mustdrop_page_config_t* c);      // partial results in the workspace
+mustdrop_status_t check_page_queries(const mustdrop_page_config_t* c);  // ... and the query rows of mustdrop_page_attend
+size_t page_attend_partial_bytes(const mustdrop_page_config_t* c);      // partial results in the workspace (of a checked configuration)
 
 }  // namespace mustdrop

@@ -156,3 +156,25 @@ def test_sizes_of_pool_and_workspace():
     assert md.mustdrop_page_workspace_bytes(md.PageConfig(n_seq=1, page=16, n_pages=1, max_pages=1, rows=1)) == 256
     with pytest.raises(TypeError):
         md.PageConfig(pages=3)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(n_q=129), dict(n_q=200), dict(n_q=-1), dict(q_heads=3), dict(q_heads=0), dict(q_heads=-4), dict(n_heads=0), dict(head_dim=96),
+    dict(n_heads=1, q_heads=129, n_q=128), dict(n_heads=1, q_heads=65536, n_q=1),
+])
+def test_no_workspace_for_queries_that_the_attention_refuses(bad):
+    cfg = md.PageConfig(**{**GOOD, **bad})
+    assert _call("attend", cfg) in (md.MUSTDROP_ERR_INVALID_ARG, md.MUSTDROP_ERR_UNSUPPORTED)
+    assert md.mustdrop_page_workspace_bytes(cfg) == 0
+
+
+def test_a_workspace_serves_every_smaller_number_of_queries():
+    for heads, q_heads in ((2, 2), (2, 4), (1, 71), (8, 64)):
+        sizes = [md.mustdrop_page_workspace_bytes(md.PageConfig(**{**GOOD, "n_heads": heads, "q_heads": q_heads, "n_q": n_q})) for n_q in range(1, 129)]
+        assert sizes[0] > 256 and sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("bad", [dict(max_q=129), dict(max_q=-1), dict(q_heads=3), dict(max_q=128, q_heads=258)])
+def test_the_owner_refuses_queries_without_a_workspace(bad):
+    with pytest.raises(md.MustDropError):      # (before anything is allocated: there is no device here)
+        md.PagedCache(**{**dict(n_seq=2, n_heads=2, n_pages=8, max_pages=4, device="cuda:0"), **bad})
