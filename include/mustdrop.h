@@ -390,6 +390,9 @@ mustdrop_status_t mustdrop_key_set(int32_t batch, int32_t n_heads, int32_t head_
  * ring state outside its limits: -1).  A bounded wait that runs out (MUSTDROP_ERR_TIMEOUT, mustdrop_page_attend) leaves outputs
  * unspecified, and the workspace has to be zeroed before it is used again.
  */
+/* Debugging: half the lanes of every warp of mustdrop_page_attend give up their first wait for a copy (exercises the time-out path). */
+#define MUSTDROP_PAGE_FLAG_DEBUG_TIMEOUT 0x10000
+
 typedef struct {
   int32_t n_seq;      /* sequences of the call, 1..65535 (mustdrop_page_attend: ..4096) */
   int32_t n_heads;    /* K / V heads, 1..65535 */
@@ -402,7 +405,7 @@ typedef struct {
   int32_t n_q;        /* attend: query tokens per sequence, 1..128 */
   int32_t causal;     /* attend: 1: query token t sees keys 0 .. len - n_q + t (the queries are the last n_q tokens); 0: all len keys */
   float   scale;      /* attend: logit scale, 0 .. 1e37; 0 => 1/sqrt(head_dim) */
-  int32_t flags;      /* must be 0 */
+  int32_t flags;      /* 0 (or the debugging bit below) */
   /* Strides in ELEMENTS (bf16); 0 => contiguous; each a multiple of 8.  Rows of head_dim elements are contiguous. */
   int64_t k_stride_s, k_stride_h, k_stride_r;   /* store: k [n_seq, n_heads, rows, head_dim] */
   int64_t v_stride_s, v_stride_h, v_stride_r;   /* store: v, likewise */

@@ -62,6 +62,7 @@ class mustdrop_config_t(ctypes.Structure):
 MUSTDROP_FLAG_REBUILD_SEQUENCE = 1
 MUSTDROP_FLAG_PER_HEAD_MAX = 2
 MUSTDROP_FLAG_INPUTS_READY = 4
+MUSTDROP_PAGE_FLAG_DEBUG_TIMEOUT = 0x10000
 
 MUSTDROP_DEBUG_VARIANT_AUTO, MUSTDROP_DEBUG_VARIANT_TWO_PASS = 0, 1
 MUSTDROP_DEBUG_VARIANT_FUSED, MUSTDROP_DEBUG_VARIANT_ROW_SPLIT = 2, 3

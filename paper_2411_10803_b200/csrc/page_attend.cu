@@ -50,6 +50,7 @@ struct AttendParams {
   uint32_t group_magic;       // 2^32 / group, rounded up: a row (below 2^14) over the group is the product's high half
   int64_t q_ss, q_st, q_sh;   // bytes
   float scale_log2e;
+  uint32_t give_up;           // lanes of a warp whose waits for copies run out at once (0, but for debugging)
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
@@ -1200,7 +1201,9 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
       while (at.left > 0) {
         const uint32_t gone = (bad >> (2 * stage)) & 3u;
         if (gone != 3u) {
-          if (!mbar_wait(bar0 + 8 * stage, (phase >> stage) & 1u)) { ok = false; break; }
+          // (one answer for the warp, as what follows needs all its lanes: every lane has a clock of its own to give up by)
+          const bool landed = mbar_wait(bar0 + 8 * stage, (phase >> stage) & 1u) && ((p.give_up >> lane) & 1u) == 0;
+          if (!__all_sync(~0u, landed)) { ok = false; break; }
           phase ^= 1u << stage;
           body.pair(p, at, ring + stage * kPair, gone);
         }
@@ -1413,6 +1416,7 @@ extern "C" mustdrop_status_t mustdrop_page_attend(const mustdrop_page_config_t* 
   p.q_ss = 2 * (c->q_stride_s != 0 ? c->q_stride_s : static_cast<int64_t>(c->n_q) * c->q_heads * c->head_dim);
   const float scale = c->scale != 0.0f ? c->scale : (c->head_dim == 128 ? 0.08838834764831845f : 0.125f);
   p.scale_log2e = scale * 1.4426950408889634f;
+  p.give_up = (c->flags & MUSTDROP_PAGE_FLAG_DEBUG_TIMEOUT) != 0 ? 0xaaaaaaaau : 0u;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);

@@ -8,7 +8,7 @@
 namespace mustdrop {
 
 mustdrop_status_t check_page_sizes(const mustdrop_page_config_t* c) {
-  if (c == nullptr || c->n_seq <= 0 || c->n_pages <= 0 || c->flags != 0) return MUSTDROP_ERR_INVALID_ARG;
+  if (c == nullptr || c->n_seq <= 0 || c->n_pages <= 0 || (c->flags & ~MUSTDROP_PAGE_FLAG_DEBUG_TIMEOUT) != 0) return MUSTDROP_ERR_INVALID_ARG;
   if (page_log2(c->page) < 0 || c->n_seq > 65535) return MUSTDROP_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(c->n_pages) * c->page > INT32_MAX) return MUSTDROP_ERR_UNSUPPORTED;
   return MUSTDROP_OK;
