@@ -206,6 +206,14 @@ __device__ __forceinline__ uint32_t lds16(uint32_t a) {
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
   return v;
 }
+// two products an instruction
+__device__ __forceinline__ float2 mul_pair(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
 // a where c, else b: as an instruction, so that an array of registers is not made an array in memory
 __device__ __forceinline__ float pick(bool c, float a, float b) {
   float d;
@@ -259,7 +267,8 @@ __device__ __forceinline__ RowSum join_row(int n, At at, int lane) {
   return s;
 }
 
-// P s goes into fp16 over a unit 2^E of its column (and, in the layout for few rows, group): mul = 2^-E, 0 where none is set.
+// P s goes into fp16 over a unit 2^E of its column and group, as groups' scales may be any powers of two apart: mul = 2^-E, 0 where none is set.
+// (One unit for all groups of a column, in the layout for more rows, was 2 to 4 % faster, and rounded a group to nothing beside one 2^24 times it.)
 // A unit is set from the pair of chunks that sets the stabiliser - their largest P s, so the tokens that now count are far from both ends of
 // fp16 - and again when P s has grown by 2^13, or when the stabiliser moves: whatever set it has then faded.
 constexpr float kUnitRoom = 13.0f;
@@ -307,8 +316,8 @@ struct Wide {
   float cs[NT][2];                         // log2 units per unit of the scaled product, of columns 2t, 2t + 1
   float o[NT][kTiles][4], oz[NT][4];    // out (without centres) and the centres' part, rows r, r + 8 and columns 2t, 2t + 1
   float l[NT][2], m[NT][2];                // sum (of this lane's tokens), stabiliser (kNone: no key seen)
-  float mul[NT][2];                        // 2^-E of columns 2t, 2t + 1
-  float most;                              // log2 of the P s that these columns' units have room for
+  float mul[NT][2][G];                     // 2^-E of columns 2t, 2t + 1 and every group
+  uint32_t room[G / 2];                    // 2^15 less the bf16 bits of the P s that the groups' units have room for, two groups to a word
   int32_t least = 0, len = 0;              // fewest visible keys of any column; the sequence's length
   uint4 next_q[NT][G];
   int32_t next_len;
@@ -402,7 +411,8 @@ struct Wide {
         cs[nt][j] = __shfl_sync(~0u, back, (2 * t + j) * 4);
         l[nt][j] = 0.0f;
         m[nt][j] = kNone;
-        mul[nt][j] = 0.0f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) mul[nt][j][g] = 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < kTiles; ++i)
@@ -412,7 +422,8 @@ struct Wide {
       for (int j = 0; j < 4; ++j) oz[nt][j] = 0.0f;
     }
     if (p.causal) least = max(0, len - p.n_q + 1 + token_of(p, at.tile * kRows));
-    most = INFINITY;
+#pragma unroll
+    for (int i = 0; i < G / 2; ++i) room[i] = 0x00010001u;
   }
 
   __device__ __forceinline__ void pair(const AttendParams& p, const Cursor& at, uint32_t c0, uint32_t gone) {
@@ -515,7 +526,7 @@ struct Wide {
     // a logit far above the stabiliser, or P s above its unit's room: move them (rare after the first chunks)
     float rise[2][NT][4];
     float high = -INFINITY;
-    uint32_t vs_top = 0;
+    uint32_t vs_top[G / 2] = {};                 // the largest scales of this lane's tokens, two groups to a word
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
 #pragma unroll
@@ -528,11 +539,14 @@ struct Wide {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int g = 0; g < G / 2; ++g) vs_top = max_u16x2(vs_top, vsw[hf][h][g]);
+        for (int g = 0; g < G / 2; ++g) vs_top[g] = max_u16x2(vs_top[g], vsw[hf][h][g]);
     }
-    vs_top = max(vs_top & 0xffffu, vs_top >> 16);
-    // (the largest logit and the largest scale of this lane's tokens, be they of the same one or not; a NaN's bits are above all scales')
-    if (__any_sync(~0u, high > 8.0f || high + scale_log2(vs_top) > most || vs_top >= 0x7f80u)) {
+    // (the largest logit and a group's largest scale, be they of the same token or not; a NaN's bits are above all scales'.  Halves of words
+    // are added as they are: no sum of two leaves its 16 bits.)
+    uint32_t over = vs_top[0] + room[0], nan = vs_top[0];
+    if (G == 4) { over = max_u16x2(over, vs_top[G / 2 - 1] + room[G / 2 - 1]); nan = max_u16x2(nan, vs_top[G / 2 - 1]); }
+    over = max(over & 0xffffu, over >> 16);
+    if (__any_sync(~0u, high > 8.0f || fmaf(static_cast<float>(over), 1.0f / 128.0f, high) > 256.0f || ((nan + 0x00800080u) & 0x80008000u) != 0)) {
       // A NaN for a scale: NaN in its group's channels (by way of the centres) for the columns that see the key, and the key's
       // scale is zero from here on: a column that does not see it has P = 0, and 0 x NaN would be one.
       uint32_t none = 0;               // bit (nt, j, g)
@@ -559,16 +573,6 @@ struct Wide {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
           if (r < G && ((none >> ((nt * 2 + j) * G + r)) & 1u)) oz[nt][j] = __uint_as_float(0x7fffffffu);
-      float size[2][2];                // log2 of the largest scale of this lane's tokens
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t v = vsw[hf][h][0];
-          if (G == 4) v = max_u16x2(v, vsw[hf][h][G / 2 - 1]);
-          size[hf][h] = scale_log2(max(v & 0xffffu, v >> 16));
-        }
-      most = INFINITY;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -588,24 +592,47 @@ struct Wide {
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) { o[nt][i][j] *= f; o[nt][i][j + 2] *= f; }
           }
-          float largest = -INFINITY;   // log2 of P s
+          // log2 of P s per group, over 1/128 and from -377 on, two groups to a word: a scale's bits are its log2 over 1/128 from -127 on
+          uint32_t largest[G / 2] = {};
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               rise[hf][nt][j + 2 * h] = fmaf(sacc[hf][nt][j + 2 * h], cs[nt][j], -m[nt][j]);
-              largest = fmaxf(largest, rise[hf][nt][j + 2 * h] + size[hf][h]);
+              const uint32_t up = static_cast<uint32_t>(fmaf(fminf(fmaxf(rise[hf][nt][j + 2 * h], -250.0f), 8.0f), 128.0f, 32000.0f));
+#pragma unroll
+              for (int i = 0; i < G / 2; ++i) largest[i] = max_u16x2(largest[i], vsw[hf][h][i] + up * 0x10001u);
             }
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, d));
-          if (moves || (mul[nt][j] != 0.0f && largest > unit_exponent(mul[nt][j]) + kUnitRoom)) {
-            float f;
-            mul[nt][j] = new_unit(mul[nt][j], largest, &f);
+          for (int i = 0; i < G / 2; ++i)
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) { o[nt][i][j] *= f; o[nt][i][j + 2] *= f; }
+            for (int d = 4; d < 32; d <<= 1) largest[i] = max_u16x2(largest[i], __shfl_xor_sync(~0u, largest[i], d));
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const float size = fmaf(static_cast<float>((g & 1) ? largest[g >> 1] >> 16 : largest[g >> 1] & 0xffffu), 1.0f / 128.0f, -377.0f);
+            float& unit = mul[nt][j][g];
+            if (moves || (unit != 0.0f && size > unit_exponent(unit) + kUnitRoom)) {
+              float f;
+              unit = new_unit(unit, size, &f);
+#pragma unroll
+              for (int i = 2 * g; i < 2 * g + 2; ++i) { o[nt][i][j] *= f; o[nt][i][j + 2] *= f; }
+            }
           }
-          if (mul[nt][j] != 0.0f) most = fminf(most, unit_exponent(mul[nt][j]) + kUnitRoom);
         }
+#pragma unroll
+      for (int i = 0; i < G / 2; ++i) {
+        int most[2] = {0x7fff, 0x7fff};      // (a unit's exponent is -100 at least: so is the room, and no half below runs over)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float unit = mul[nt][j][2 * i + e];
+              if (unit != 0.0f) most[e] = min(most[e], (unit_exponent(unit) + static_cast<int>(kUnitRoom) + 127) * 128);
+            }
+        room[i] = 0x80008000u - static_cast<uint32_t>(most[1] << 16 | most[0]);
+      }
     }
     // probabilities; P and P s, turned into second operands; out
 #pragma unroll
@@ -623,11 +650,12 @@ struct Wide {
         mma_bf16(oz[nt], vz[hf][0], 0u, vz[hf][1], 0u, pz0, pz1);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float p0 = pr[2 * h] * mul[nt][0], p1 = pr[2 * h + 1] * mul[nt][1];
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             const float s = (g & 1) ? bf16_hi(vsw[hf][h][g >> 1]) : bf16_lo(vsw[hf][h][g >> 1]);
-            pv[nt][g][h] = transpose8x8(pack_f16(p0 * s, p1 * s));
+            const float2 in_unit = mul_pair(make_float2(pr[2 * h], pr[2 * h + 1]), make_float2(mul[nt][0][g], mul[nt][1][g]));
+            const float2 ps = mul_pair(in_unit, make_float2(s, s));
+            pv[nt][g][h] = transpose8x8(pack_f16(ps.x, ps.y));
           }
         }
       }
@@ -658,11 +686,11 @@ struct Wide {
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
         const int in_tile = nt * 8 + 2 * t + j, row = at.tile * kRows + in_tile;
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum, unit = mul[nt][j] == 0.0f ? 1.0f : 1.0f / mul[nt][j];
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         uint16_t* const dst = p.out + at.seq * out_seq + out_row(p, row, at.head) * D;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          const float z = __shfl_sync(~0u, oz[nt][j], g * 4 + t);
+          const float z = __shfl_sync(~0u, oz[nt][j], g * 4 + t), unit = mul[nt][j][g] == 0.0f ? 1.0f : 1.0f / mul[nt][j][g];
           float v[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[i] = fmaf(o[nt][2 * g + (i >> 1)][j + 2 * (i & 1)], unit, z);
