@@ -461,8 +461,9 @@ mustdrop_status_t mustdrop_page_load(const mustdrop_page_config_t *config /* (ho
  * q bf16 [n_seq, n_q, q_heads, head_dim] (strides); page_table int32 [n_seq, max_pages], len int32 [n_seq]: keys
  * 0 .. len[s]-1 are read through the table (clamped to [0, max_pages * page], recorded as MUSTDROP_ERR_BAD_LENGTH);
  * out bf16 [n_seq, n_q, q_heads, head_dim] contiguous.  A query token that sees no key gets zeros.  Keys on a page id
- * outside [0, n_pages) are left out and recorded as MUSTDROP_ERR_BAD_PAGE.  fp32 accumulation, probabilities in
- * 11 bits; the same call gives the same bits.
+ * outside [0, n_pages) are left out and recorded as MUSTDROP_ERR_BAD_PAGE.  fp32 accumulation; probabilities
+ * times scales are rounded to 11 bits before they meet the codes, probabilities to no fewer than 16 before they meet the centres; the same
+ * call gives the same bits.
  */
 mustdrop_status_t mustdrop_page_attend(const mustdrop_page_config_t *config /* (host) */, const void *q,
                                        const void *pool, const int32_t *page_table, const int32_t *len, void *out,

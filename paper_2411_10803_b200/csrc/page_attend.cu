@@ -646,8 +646,11 @@ struct Wide {
         for (int j = 0; j < 4; ++j) pr[j] = ex2(rise[hf][nt][j]);
         l[nt][0] += pr[0] + pr[2];
         l[nt][1] += pr[1] + pr[3];
-        const uint32_t pz0 = transpose8x8(pack_bf16(pr[0], pr[1])), pz1 = transpose8x8(pack_bf16(pr[2], pr[3]));
-        mma_bf16(oz[nt], vz[hf][0], 0u, vz[hf][1], 0u, pz0, pz1);
+        // (P in two bf16 terms, 16 bits: far from zero the centres carry the result, and the sum of P beside it is of fp32.  One term was 3 % faster.)
+        const uint32_t p0 = pack_bf16(pr[0], pr[1]), p1 = pack_bf16(pr[2], pr[3]);
+        mma_bf16(oz[nt], vz[hf][0], 0u, vz[hf][1], 0u, transpose8x8(p0), transpose8x8(p1));
+        mma_bf16(oz[nt], vz[hf][0], 0u, vz[hf][1], 0u, transpose8x8(pack_bf16(pr[0] - bf16_lo(p0), pr[1] - bf16_hi(p0))),
+                 transpose8x8(pack_bf16(pr[2] - bf16_lo(p1), pr[3] - bf16_hi(p1))));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll

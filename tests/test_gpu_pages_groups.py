@@ -3,8 +3,9 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import pages
 from paper_2411_10803_b200 import build as md_build
-from test_gpu_pages import Case, queries
+from test_gpu_pages import BF16, FP16, Case, f64, queries
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +56,46 @@ def test_groups_of_v_far_apart_in_a_sequence_that_many_ctas_share(group, n_q):
     v = rng.standard_normal((1, 1, 7001, 128)) * np.repeat(np.exp2([0, 24, -24, 48]), 32)
     c = Case(rng, [7001], heads=1, page=64, k=rng.standard_normal(v.shape), v=v)
     c.check(queries(rng, 1, n_q, group, 128))
+
+
+def bounds(c, q, causal):
+    """-> (out in 64 bits, how far a result may be off): half a step of the result; P s in fp16 times the codes; P in 11 bits times the
+    centres (it has 16, which leaves room for fp32 sums over a few hundred keys); and what a logit's error makes of the probabilities,
+    24 roundings of at most 2^-22 of its magnitudes."""
+    q = f64(q)
+    n, n_q, q_heads, d = q.shape
+    group = q_heads // c.heads
+    k, v = pages.values(c.ck, c.sk, c.zk), pages.values(c.cv, c.sv, c.zv)
+    z = np.repeat(np.abs(c.zv), 32, -1)
+    codes = np.abs(v - np.repeat(c.zv, 32, -1))
+    kz = np.repeat(np.abs(c.zk), 32, -1)
+    mass = np.abs(k - np.repeat(c.zk, 32, -1)) + kz
+    out, tol = np.zeros(q.shape), np.zeros(q.shape)
+    for s, t, j in np.ndindex(n, n_q, q_heads):
+        h, seen = j // group, int(c.lens[s]) - (n_q - 1 - t if causal else 0)
+        if seen <= 0:
+            continue
+        x = k[s, h, :seen] @ q[s, t, j] * d ** -0.5
+        p = np.exp(x - x.max())
+        p /= p.sum()
+        dz = 24 * 2.0 ** -22 * (mass[s, h, :seen] @ np.abs(q[s, t, j])).max() * d ** -0.5 + 2.0 ** -20
+        out[s, t, j] = p @ v[s, h, :seen]
+        tol[s, t, j] = BF16 * np.abs(out[s, t, j]) + (FP16 + 2 * dz) * (1 + BF16) * (p @ (codes[s, h, :seen] + z[s, h, :seen])) + 1e-30
+    return out, tol
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group,n_q", ROWS)
+def test_centres_far_from_zero_that_cancel(group, n_q, d, causal):
+    """Values of +300 and -300 in turn with a spread of one: the centres are the result, and what P loses before it meets them is not
+    made up for by its sum."""
+    rng = np.random.default_rng(n_q * group)
+    lens = [2, 3, 5, 8, 13, 40, 300, 1, 0]
+    v = rng.standard_normal((9, 2, 300, d)) + 300.0 * (-1.0) ** np.arange(300)[:, None]
+    c = Case(rng, lens, heads=2, d=d, k=0.3 * rng.standard_normal(v.shape), v=v)
+    q = queries(rng, 9, n_q, 2 * group, d)
+    out, code = c.attend(q, causal)
+    want, tol = bounds(c, q, causal)
+    off = np.abs(f64(out) - want)
+    assert code == [0, 0] and (off <= tol).all(), (off / np.maximum(tol, 1e-30)).max()
