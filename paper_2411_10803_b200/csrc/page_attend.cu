@@ -298,6 +298,12 @@ __device__ __forceinline__ const uint8_t* q_row(const AttendParams& p, int seq, 
   return p.q + seq * p.q_ss + tq * p.q_st + (static_cast<int64_t>(head) * p.group + (row - tq * p.group)) * p.q_sh;
 }
 
+// log2 units of a logit per unit of a product of q over 2^e: a number above zero and finite, as hidden keys' logits are -inf and a zero
+// key's are zero (a scale below 2^-37 over a q of zeros would be none: NaN)
+__device__ __forceinline__ float log2_per_product(const AttendParams& p, int e) {
+  return fminf(fmaxf(__uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.scale_log2e, __uint_as_float(1u)), 3.4e38f);
+}
+
 constexpr float kNone = -3.0e38f;   // stabiliser of a column that has seen no key
 
 // What a warp holds of the unit in hand, and its arithmetic, for up to 8 NT query rows: a column each.
@@ -364,7 +370,7 @@ struct Wide {
       // largest member to [2^14, 2^15)
       const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);
       const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
-      const float back = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * p.scale_log2e;
+      const float back = log2_per_product(p, e - 14);
       float sums[G], offs[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
@@ -764,7 +770,7 @@ struct Narrow {
     top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
     const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);   // largest member to [2^14, 2^15)
     const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
-    const float back = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23) * p.scale_log2e;
+    const float back = log2_per_product(p, e - 14);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] *= up;
     const float odd = (f[1] + f[3]) + (f[5] + f[7]), even = (f[0] + f[2]) + (f[4] + f[6]);

@@ -35,3 +35,21 @@ def test_a_wait_that_runs_out_in_some_lanes_ends_the_call(d, lens, heads, group,
         assert not out[empty].any()                 # (zeros of sequences without keys wait for nothing)
         ws.zero_()
         c.check(q, ws=ws)
+
+
+@pytest.mark.parametrize("scale", [1e-7, 1e-12, 1e-25, 1e-38, 1e-44])
+@pytest.mark.parametrize("group,n_q", [(1, 1), (2, 1), (4, 1), (3, 5)])
+def test_scales_down_to_the_smallest_there_is(scale, group, n_q):
+    """Every visible key has the same share, hidden ones none - for queries of zeros (a padded row) as well."""
+    c = Case(np.random.default_rng(3), [37, 5, 0, 600], heads=2, d=128)
+    q = queries(np.random.default_rng(4), 4, n_q, 2 * group, 128)
+    q[:, :, ::2] = 0
+    c.check(q, scale=scale)
+    c.check(torch.zeros_like(q), scale=scale, causal=False)
+
+
+def test_the_largest_scale_over_keys_of_zeros():
+    rng = np.random.default_rng(5)
+    c = Case(rng, [50], heads=1, d=64, k=np.zeros((1, 1, 50, 64)), v=rng.standard_normal((1, 1, 50, 64)))
+    for rows in (1, 2, 5):
+        c.check(queries(rng, 1, 2, rows, 64, 3e7), scale=1e37)
