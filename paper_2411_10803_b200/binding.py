@@ -514,7 +514,8 @@ class PagedCache:
 
     n_seq sequences (one per layer and request: layer * batch + request, say) of n_heads K / V heads share n_pages pages.
     All arithmetic happens in the library calls; this class only allocates and forwards.  Its calls share one workspace:
-    they belong on one stream, or on streams that wait for each other.
+    they belong on one stream, or on streams that wait for each other.  `stream` (a torch stream or a raw handle) is the current one by
+    default; a call on another one orders nothing between the two, but tensors dropped after it are not handed out again too early.
     """
 
     def __init__(self, n_seq, n_heads, n_pages, max_pages, head_dim=128, page=16, q_heads=None, max_q=1, causal=1, scale=0.0,
@@ -557,6 +558,34 @@ class PagedCache:
         import torch
         return torch.cuda.device(self.device)
 
+    def _other(self, stream):
+        """The torch stream of `stream`, if that is not the device's current one."""
+        import torch
+        if stream is None:
+            return None
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
+        return None if stream.cuda_stream == torch.cuda.current_stream(self.device).cuda_stream else stream
+
+    def _empty(self, shape, dtype, stream):
+        """A result of a call on `stream`: memory of that stream, which nothing still pending on the current one uses."""
+        import torch
+        other = self._other(stream)
+        if other is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(other):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(torch.cuda.current_stream(self.device))
+        return t
+
+    def _lend(self, stream, *tensors):
+        """The caller's tensors, which a call on `stream` uses: dropped before it has, they are not handed out again."""
+        other = self._other(stream)
+        if other is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(other)
+
     @staticmethod
     def _want(t, shape, name):
         import torch
@@ -579,10 +608,11 @@ class PagedCache:
         if add.dtype != torch.int32 or add.numel() != self.n_seq or not add.is_contiguous():
             raise ValueError("add: contiguous int32 [%d] expected" % self.n_seq)
         if slots is None:
-            slots = torch.empty((self.n_seq, rows), dtype=torch.int32, device=self.device)
+            slots = self._empty((self.n_seq, rows), torch.int32, stream)
         elif slots.dtype != torch.int32 or tuple(slots.shape) != (self.n_seq, rows) or not slots.is_contiguous():
             raise ValueError("slots: contiguous int32 [%d, %d] expected" % (self.n_seq, rows))
         self._check(None, "extend", (add, slots))
+        self._lend(stream, add, slots)
         c = self._config(("extend", rows), n_seq=self.n_seq, rows=rows, **self._base)
         with self._on():
             st = mustdrop_page_tables(c, add, self.len, self.ring_state, self.len, self.ring_state, self.ring, self.page_table,
@@ -602,6 +632,7 @@ class PagedCache:
         for name, t in (("k", k), ("v", v)):
             self._want(t, (n, self.n_heads, rows, self.head_dim), name)
         self._check(None, "store", (slots, k, v))
+        self._lend(stream, slots, k, v)
         ks, vs = self._strides(k, "k"), self._strides(v, "v")
         c = self._config(("store", n, rows, ks, vs), n_seq=n, rows=rows, k_stride_s=ks[0], k_stride_h=ks[1], k_stride_r=ks[2],
                          v_stride_s=vs[0], v_stride_h=vs[1], v_stride_r=vs[2], **self._base)
@@ -618,6 +649,7 @@ class PagedCache:
                 if not t.is_contiguous():
                     raise ValueError("%s: contiguous rows expected" % name)
         self._check(None, "load", (slots, k_out, v_out))
+        self._lend(stream, slots, k_out, v_out)
         c = self._config(("load", n, rows), n_seq=n, rows=rows, **self._base)
         with self._on():
             st = mustdrop_page_load(c, slots, self.pool, k_out, v_out, self.workspace, stream)
@@ -632,11 +664,12 @@ class PagedCache:
         if n_q > self.max_q or first < 0 or first + n > self.n_seq:
             raise ValueError("attend: at most %d query tokens of sequences 0 .. %d" % (self.max_q, self.n_seq - 1))
         if out is None:
-            out = torch.empty((n, n_q, self.q_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
+            out = self._empty((n, n_q, self.q_heads, self.head_dim), torch.bfloat16, stream)
         self._want(out, (n, n_q, self.q_heads, self.head_dim), "out")
         if not out.is_contiguous():
             raise ValueError("out: contiguous rows expected")
         self._check(None, "attend", (q, out))
+        self._lend(stream, q, out)
         qs = self._strides(q, "q")
         c = self._config(("attend", n, n_q, qs), n_seq=n, n_q=n_q, q_stride_s=qs[0], q_stride_t=qs[1], q_stride_h=qs[2], **self._attend)
         with self._on():

@@ -53,3 +53,69 @@ def test_the_largest_scale_over_keys_of_zeros():
     c = Case(rng, [50], heads=1, d=64, k=np.zeros((1, 1, 50, 64)), v=rng.standard_normal((1, 1, 50, 64)))
     for rows in (1, 2, 5):
         c.check(queries(rng, 1, 2, rows, 64, 3e7), scale=1e37)
+
+
+LONG = 40_000_000      # clock cycles that hold a stream up: some 20 ms
+
+
+def filled(n, heads=2, rows=40):
+    cache = md.PagedCache(n_seq=n, n_heads=heads, n_pages=8 * n, max_pages=8, max_q=2)
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    k, v = (torch.randn((n, heads, rows, 128), device="cuda", generator=gen).bfloat16() for _ in range(2))
+    cache.store(cache.extend(torch.full((n,), rows, dtype=torch.int32, device="cuda"), rows), k, v)
+    cache.attend(torch.zeros((n, 1, heads, 128), dtype=torch.bfloat16, device="cuda"))     # (first calls take longer than the delay)
+    torch.cuda._sleep(1000)
+    return cache
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_results_of_a_call_on_another_stream_are_not_handed_out_again(raw):
+    cache = filled(64)
+    q = queries(np.random.default_rng(1), 64, 1, 2, 128)
+    side = torch.cuda.Stream()
+    on = side.cuda_stream if raw else side
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(LONG)
+    out = cache.attend(q, stream=on)                   # pending behind the delay, and dropped
+    slots = cache.extend(torch.zeros(64, dtype=torch.int32, device="cuda"), 37, stream=on)
+    del out, slots
+    ours = [torch.full((64, 1, 2, 128), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    more = [torch.full((64, 37), 9, dtype=torch.int32, device="cuda") for _ in range(3)]
+    torch.cuda.synchronize()
+    assert all((x == 5).all() for x in ours) and all((x == 9).all() for x in more)
+    assert cache.device_status() == (0, 0)
+
+
+def test_results_of_a_call_on_another_stream_use_no_memory_still_read_on_this_one():
+    cache = filled(64)
+    q = queries(np.random.default_rng(1), 64, 1, 2, 128)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    before, copy = torch.full((64, 1, 2, 128), 3.0, dtype=torch.bfloat16, device="cuda"), torch.zeros_like(q)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(LONG)
+    copy.copy_(before)                                 # pending on the current stream, and its source dropped
+    del before
+    out = cache.attend(q, stream=side)
+    torch.cuda.synchronize()
+    assert (copy == 3).all()
+    assert torch.equal(out, cache.attend(q))
+
+
+def test_arguments_of_a_call_on_another_stream_may_be_dropped():
+    cache = filled(64)
+    q = queries(np.random.default_rng(1), 64, 1, 2, 128)
+    want = cache.attend(q)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(LONG)
+    out, mine = torch.zeros_like(q), q.clone()
+    side.wait_stream(torch.cuda.current_stream())
+    cache.attend(mine, out=out, stream=side)
+    del mine
+    others = [torch.full_like(q, 50.0) for _ in range(3)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and all((x == 50).all() for x in others)
