@@ -677,7 +677,8 @@ class PagedCache:
         self._check(st, "mustdrop_page_attend", ())
         return out
 
-    def device_status(self):
-        """(code, detail) the calls so far recorded (synchronises)."""
+    def device_status(self, stream=None):
+        """(code, detail) that the calls so far on `stream` recorded (synchronises it)."""
         import torch
-        return tuple(self.workspace[:8].view(torch.int32).tolist())
+        with self._on(), torch.cuda.stream(self._other(stream)):
+            return tuple(self.workspace[:8].view(torch.int32).tolist())

@@ -119,3 +119,17 @@ def test_arguments_of_a_call_on_another_stream_may_be_dropped():
     others = [torch.full_like(q, 50.0) for _ in range(3)]
     torch.cuda.synchronize()
     assert torch.equal(out, want) and all((x == 50).all() for x in others)
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_the_status_of_another_stream_is_read_behind_its_calls(raw):
+    cache = filled(3)
+    side = torch.cuda.Stream()
+    on = side.cuda_stream if raw else side
+    add, slots = torch.tensor([1, 9, 1], dtype=torch.int32, device="cuda"), torch.empty((3, 1), dtype=torch.int32, device="cuda")
+    assert cache.device_status() == cache.device_status(on) == (0, 0)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(LONG)
+    cache.extend(add, 1, slots, stream=on)             # more tokens than rows for sequence 1
+    assert cache.device_status(on) == (md.MUSTDROP_ERR_BAD_LENGTH, 1)
+    assert cache.device_status() == (md.MUSTDROP_ERR_BAD_LENGTH, 1) and cache.len.tolist() == [41, 40, 41]
