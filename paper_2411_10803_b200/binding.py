@@ -677,8 +677,12 @@ class PagedCache:
         self._check(st, "mustdrop_page_attend", ())
         return out
 
-    def device_status(self, stream=None):
-        """(code, detail) that the calls so far on `stream` recorded (synchronises it)."""
+    def device_status(self, stream=None, clear=False):
+        """(code, detail) of the first condition that the calls so far on `stream` recorded (synchronises it).  It stays, and hides later ones,
+        until `clear`, which makes the workspace fit for use again after MUSTDROP_ERR_TIMEOUT too."""
         import torch
         with self._on(), torch.cuda.stream(self._other(stream)):
-            return tuple(self.workspace[:8].view(torch.int32).tolist())
+            found = tuple(self.workspace[:8].view(torch.int32).tolist())
+            if clear:
+                self.workspace.zero_()
+        return found

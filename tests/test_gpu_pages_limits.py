@@ -133,3 +133,26 @@ def test_the_status_of_another_stream_is_read_behind_its_calls(raw):
     cache.extend(add, 1, slots, stream=on)             # more tokens than rows for sequence 1
     assert cache.device_status(on) == (md.MUSTDROP_ERR_BAD_LENGTH, 1)
     assert cache.device_status() == (md.MUSTDROP_ERR_BAD_LENGTH, 1) and cache.len.tolist() == [41, 40, 41]
+
+
+def test_a_status_that_was_cleared_does_not_hide_the_next():
+    cache = md.PagedCache(n_seq=3, n_heads=2, n_pages=4, max_pages=8, max_q=2)
+    i = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    rows = queries(np.random.default_rng(2), 3, 2, 16, 128)
+    cache.store(cache.extend(i(16, 16, 16), 16), rows, rows)
+    cache.extend(i(0, 33, 0), 40)                      # two pages asked for, one is free
+    assert cache.device_status() == (md.MUSTDROP_ERR_NO_PAGES, 1) and cache.len.tolist() == [16, 16, 16]
+    cache.extend(i(0, 0, 41), 40)                      # more tokens than rows: hidden behind the first
+    assert cache.device_status(clear=True) == (md.MUSTDROP_ERR_NO_PAGES, 1)
+    assert cache.device_status() == (0, 0)
+    cache.extend(i(0, 0, 41), 40)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    assert cache.device_status(side, clear=True) == (md.MUSTDROP_ERR_BAD_LENGTH, 2)
+    torch.cuda.current_stream().wait_stream(side)
+    q = queries(np.random.default_rng(1), 3, 1, 2, 128)
+    out = cache.attend(q)
+    assert cache.device_status(clear=True) == cache.device_status() == (0, 0)
+    cache.workspace[:1024] = 255                       # what a call that timed out may leave: a status and counters
+    assert cache.device_status(clear=True)[0] != 0
+    assert torch.equal(out, cache.attend(q)) and cache.device_status() == (0, 0)
