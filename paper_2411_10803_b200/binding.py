@@ -544,6 +544,8 @@ class PagedCache:
     def _config(self, key, **sizes):
         c = self._configs.get(key)
         if c is None:
+            if len(self._configs) >= 256:      # (a server's prompts have ever other lengths; calls in flight have read theirs)
+                self._configs.clear()
             c = self._configs[key] = PageConfig(**sizes)
         return c
 

@@ -178,3 +178,12 @@ def test_a_workspace_serves_every_smaller_number_of_queries():
 def test_the_owner_refuses_queries_without_a_workspace(bad):
     with pytest.raises(md.MustDropError):      # (before anything is allocated: there is no device here)
         md.PagedCache(**{**dict(n_seq=2, n_heads=2, n_pages=8, max_pages=4, device="cuda:0"), **bad})
+
+
+def test_the_owner_keeps_a_bounded_number_of_descriptors():
+    cache = object.__new__(md.PagedCache)
+    cache._configs = {}
+    for rows in list(range(1, 2000)) * 2:
+        c = cache._config(("extend", rows), n_seq=3, rows=rows, n_pages=4)
+        assert c.c.rows == rows and c is cache._config(("extend", rows), n_seq=3, rows=rows, n_pages=4)
+    assert len(cache._configs) <= 256
