@@ -463,7 +463,8 @@ mustdrop_status_t mustdrop_page_load(const mustdrop_page_config_t *config /* (ho
  * out bf16 [n_seq, n_q, q_heads, head_dim] contiguous.  A query token that sees no key gets zeros.  Keys on a page id
  * outside [0, n_pages) are left out and recorded as MUSTDROP_ERR_BAD_PAGE.  fp32 accumulation; probabilities
  * times scales are rounded to 11 bits before they meet the codes, probabilities to no fewer than 16 before they meet the centres; the same
- * call gives the same bits.
+ * call gives the same bits.  Logits are to stay below 2^24, members of q
+ * times the scale below 2^116: beyond that results are unspecified.
  */
 mustdrop_status_t mustdrop_page_attend(const mustdrop_page_config_t *config /* (host) */, const void *q,
                                        const void *pool, const int32_t *page_table, const int32_t *len, void *out,

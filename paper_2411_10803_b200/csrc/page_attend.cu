@@ -8,9 +8,9 @@
 // so the codes go into the matrix instructions as they are, with 16 tokens (K) or 16 channels (V) as the rows and the query
 // rows - the query tokens and heads that share a K / V head - as the 8 columns.  Scales meet fp32 accumulators (K) or
 // the probabilities (V).  Codes are fp16 operands (exact); q is scaled by a power of two into fp16's range (exact but for
-// members below 2^-29 of the largest); P s is rounded once, to 11 bits, with a running power of two that keeps it in fp16's
-// range whatever the scales are.  A word of eight codes is five instructions of bits, and four more where the offset of its operands is
-// taken off one by one.  K's is taken off the sums instead (offsets_of).  Not V's: the matrix instruction's fp32 sums are cut, not
+// members below 2^-27 of the largest); P s is rounded once, to 11 bits, with a running power of two per query row and group that keeps it
+// in fp16's range whatever the scales are.  A word of eight codes is five instructions of bits, and four more where the offset of its operands is
+// taken off one by one.  K's is taken off the sums instead (kCodeUnit).  Not V's: the matrix instruction's fp32 sums are cut, not
 // rounded, so an offset of 1032 P s in a sum over many tokens leaves a bias (4.5e-3 of the result, 1.6e-3 being bf16's own rounding, over
 // 1000 tokens with the offset taken off every 512).  (e4m3 operands, in which a code is a code's own bits, were slower: this GPU runs that
 // instruction as two of fp16 behind conversions.)
@@ -94,9 +94,17 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
   return w;
 }
-// K's codes are operands with their offsets: 1024 + c for even channels, 1024 + 16 c over a q that is divided by 16 for odd ones.  What takes
-// them off again, for codes - 8: a sum over q alone.  (Costs some eight bits of the 24 that the products' sums have: 2e-5 of a logit's spread.)
-__device__ __forceinline__ float offsets_of(float even, float odd) { return fmaf(-1032.0f, even, -72.0f * odd); }
+// K's codes are operands as they are, as subnormal numbers: c 2^-24 for even channels, 16 c 2^-24 over a q that is divided by 16 for odd
+// ones, so a logit's sums are in units of 2^-24.  What takes 8 off the codes is a sum over q alone.  (An offset of 1024 under the codes, taken off
+// the same way, cost seven bits of the sums: 5 % of the result where 8000 nats of products cancel, three and more query rows.  What the unit costs is range at one end and gives at
+// the other: keys up to the type's largest, queries up to 2^116 over the scale.)
+constexpr float kCodeUnit = 0x1p-24f;
+constexpr int kCodeLog2 = 24;
+__device__ __forceinline__ uint32_t times_minus8(uint32_t sums) {   // of a bf16 pair
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(sums), "r"(0xc100c100u));
+  return d;
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   uint32_t d;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
@@ -112,8 +120,7 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Nibbles j and j + 4 of a word as fp16 pairs, for j = 0..3.  A nibble under the bits of 1024 reads 1024 + c (bits 0..3) or 1024 + 16 c
-// (bits 4..7); CODES takes either offset off, in one exact operation a pair.
+// Nibbles j and j + 4 of a word as fp16 pairs, for j = 0..3: the fields of a word that a mask leaves, as K takes them, ...
 struct Consts {   // kept in registers: as literals the compiler loads them again for every word
   uint32_t low, high, magic, sixteenth, minus72;
 };
@@ -122,21 +129,24 @@ __device__ __forceinline__ uint32_t opaque(uint32_t v) {
   return v;
 }
 __device__ __forceinline__ Consts make_consts() {
-  return {opaque(0x000f000fu), opaque(0x00f000f0u), opaque(0x64006400u), opaque(0x2c002c00u), opaque(0xd480d480u)};   // .., 1/16, -72
+  return {opaque(0x000f000fu), opaque(0x00f000f0u), opaque(0x64006400u), opaque(0x2c002c00u), opaque(0xd480d480u)};   // .., 1024, 1/16, -72
 }
-template <bool CODES>
-__device__ __forceinline__ void unpack8(const Consts& k, uint32_t w, uint32_t (&x)[4]) {
+__device__ __forceinline__ void nibbles8(const Consts& k, uint32_t w, uint32_t (&x)[4]) {
+  const uint32_t w8 = w >> 8;
+  x[0] = w & k.low; x[1] = w & k.high; x[2] = w8 & k.low; x[3] = w8 & k.high;
+}
+// ... and less 8, as V does.  (The well-known way from four bits to fp16: a nibble under the bits of 1024 reads 1024 + c, or 1024 + 16 c in bits
+// 4..7, and one exact operation a pair takes the rest off.)
+__device__ __forceinline__ void codes8(const Consts& k, uint32_t w, uint32_t (&x)[4]) {
   const uint32_t w8 = w >> 8;
   asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[0]) : "r"(w), "r"(k.low), "r"(k.magic));
   asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[1]) : "r"(w), "r"(k.high), "r"(k.magic));
   asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[2]) : "r"(w8), "r"(k.low), "r"(k.magic));
   asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[3]) : "r"(w8), "r"(k.high), "r"(k.magic));
-  if (CODES) {
-    asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(x[0]) : "r"(0x64086408u));                              // 1032
-    asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(x[1]) : "r"(k.sixteenth), "r"(k.minus72));
-    asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(x[2]) : "r"(0x64086408u));
-    asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(x[3]) : "r"(k.sixteenth), "r"(k.minus72));
-  }
+  asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(x[0]) : "r"(0x64086408u));                              // 1032
+  asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(x[1]) : "r"(k.sixteenth), "r"(k.minus72));
+  asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(x[2]) : "r"(0x64086408u));
+  asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(x[3]) : "r"(k.sixteenth), "r"(k.minus72));
 }
 
 // The line of chunks: sequence s has heads * tiles units of chunks(s) chunks each.
@@ -301,7 +311,7 @@ __device__ __forceinline__ const uint8_t* q_row(const AttendParams& p, int seq, 
 // log2 units of a logit per unit of a product of q over 2^e: a number above zero and finite, as hidden keys' logits are -inf and a zero
 // key's are zero (a scale below 2^-37 over a q of zeros would be none: NaN)
 __device__ __forceinline__ float log2_per_product(const AttendParams& p, int e) {
-  return fminf(fmaxf(__uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.scale_log2e, __uint_as_float(1u)), 3.4e38f);
+  return fminf(fmaxf(ldexpf(p.scale_log2e, e), __uint_as_float(1u)), 3.4e38f);
 }
 
 constexpr float kNone = -3.0e38f;   // stabiliser of a column that has seen no key
@@ -370,8 +380,8 @@ struct Wide {
       // largest member to [2^14, 2^15)
       const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);
       const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
-      const float back = log2_per_product(p, e - 14);
-      float sums[G], offs[G];
+      const float back = log2_per_product(p, e - 14 + kCodeLog2);
+      float sums[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const uint32_t ww[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
@@ -380,38 +390,31 @@ struct Wide {
         for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(ww[i]) * up; f[2 * i + 1] = bf16_hi(ww[i]) * up; }
 #pragma unroll
         for (int i = 0; i < 4; ++i) qf[nt][g][i] = (i & 1) ? pack_f16(f[i] * 0.0625f, f[i + 4] * 0.0625f) : pack_f16(f[i], f[i + 4]);
-        const float odd = (f[1] + f[3]) + (f[5] + f[7]), even = (f[0] + f[2]) + (f[4] + f[6]);
-        float s = odd + even, off = offsets_of(even, odd);
+        float s = (((f[1] + f[3]) + (f[5] + f[7])) + ((f[0] + f[2]) + (f[4] + f[6]))) * kCodeUnit;
         s += __shfl_xor_sync(~0u, s, 1);
         s += __shfl_xor_sync(~0u, s, 2);
-        off += __shfl_xor_sync(~0u, off, 1);
-        off += __shfl_xor_sync(~0u, off, 2);
         sums[g] = s;
-        offs[g] = off;
       }
       // terms of the sums: operand slots 4 term + g (two groups: 2 term + g); lane t holds slots 2t, 2t + 1 and 2t + 8, 2t + 9.
       // (A q that holds an infinity or a NaN has one in its sums: its logits are none either.)
       const bool high = (G == 4) && (t & 1);
+      float a = high ? sums[G - 2] : sums[0], b = high ? sums[G - 1] : sums[1];
+      uint32_t term[3];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float a = k == 0 ? (high ? sums[G - 2] : sums[0]) : (high ? offs[G - 2] : offs[0]);
-        float b = k == 0 ? (high ? sums[G - 1] : sums[1]) : (high ? offs[G - 1] : offs[1]);
-        uint32_t term[3];
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-          term[i] = pack_bf16(a, b);
-          a -= bf16_lo(term[i]);
-          b -= bf16_hi(term[i]);
-        }
-        uint32_t* const to = k == 0 ? qz[nt] : qs[nt];
-        if (G == 4) {
-          to[0] = t < 2 ? term[0] : term[1];
-          to[1] = t < 2 ? term[2] : 0u;
-        } else {
-          to[0] = t == 0 ? term[0] : t == 1 ? term[1] : t == 2 ? term[2] : 0u;
-          to[1] = 0u;
-        }
+      for (int i = 0; i < 3; ++i) {
+        term[i] = pack_bf16(a, b);
+        a -= bf16_lo(term[i]);
+        b -= bf16_hi(term[i]);
       }
+      if (G == 4) {
+        qz[nt][0] = t < 2 ? term[0] : term[1];
+        qz[nt][1] = t < 2 ? term[2] : 0u;
+      } else {
+        qz[nt][0] = t == 0 ? term[0] : t == 1 ? term[1] : t == 2 ? term[2] : 0u;
+        qz[nt][1] = 0u;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) qs[nt][i] = times_minus8(qz[nt][i]);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         cs[nt][j] = __shfl_sync(~0u, back, (2 * t + j) * 4);
@@ -474,8 +477,8 @@ struct Wide {
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         uint32_t u0[4], u1[4];
-        unpack8<false>(consts, kw[0][g], u0);
-        unpack8<false>(consts, kw[1][g], u1);
+        nibbles8(consts, kw[0][g], u0);
+        nibbles8(consts, kw[1][g], u1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -675,7 +678,7 @@ struct Wide {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t u[4];
-          unpack8<true>(consts, ww[i], u);
+          codes8(consts, ww[i], u);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
             mma_f16(o[nt][4 * a + i], u[0], u[1], u[2], u[3], pv[nt][2 * a + (i >> 1)][0], pv[nt][2 * a + (i >> 1)][1]);
@@ -770,15 +773,13 @@ struct Narrow {
     top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
     const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 0xff) - 127, -98), 127);   // largest member to [2^14, 2^15)
     const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
-    const float back = log2_per_product(p, e - 14);
+    const float back = log2_per_product(p, e - 14 + kCodeLog2);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] *= up;
-    const float odd = (f[1] + f[3]) + (f[5] + f[7]), even = (f[0] + f[2]) + (f[4] + f[6]);
-    float sum = odd + even, off = offsets_of(even, odd);
+    float sum = (((f[1] + f[3]) + (f[5] + f[7])) + ((f[0] + f[2]) + (f[4] + f[6]))) * kCodeUnit;
     sum += __shfl_xor_sync(~0u, sum, 1);
     sum += __shfl_xor_sync(~0u, sum, 2);
-    off += __shfl_xor_sync(~0u, off, 1);
-    off += __shfl_xor_sync(~0u, off, 2);
+    const float off = -8.0f * sum;
     const bool used = R == 2 || (n & 1) == 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -828,8 +829,8 @@ struct Narrow {
 #pragma unroll
       for (int i = 0; i < G; ++i) {
         uint32_t u0[4], u1[4];
-        unpack8<false>(consts, kw[0][i], u0);
-        unpack8<false>(consts, kw[1][i], u1);
+        nibbles8(consts, kw[0][i], u0);
+        nibbles8(consts, kw[1][i], u1);
         mma_f16(a, u0[0], u1[0], u0[1], u1[1], qf[i][0], qf[i][1]);
         mma_f16(a, u0[2], u1[2], u0[3], u1[3], qf[i][2], qf[i][3]);
       }
@@ -947,7 +948,7 @@ struct Narrow {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t u[4];
-          unpack8<true>(consts, ww[i], u);
+          codes8(consts, ww[i], u);
           mma_f16(o[4 * a + i], u[0], u[1], u[2], u[3], pv[0], pv[1]);
         }
       }

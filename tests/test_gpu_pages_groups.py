@@ -99,3 +99,41 @@ def test_centres_far_from_zero_that_cancel(group, n_q, d, causal):
     want, tol = bounds(c, q, causal)
     off = np.abs(f64(out) - want)
     assert code == [0, 0] and (off <= tol).all(), (off / np.maximum(tol, 1e-30)).max()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group,n_q", ROWS)
+def test_products_of_keys_that_cancel(group, n_q, d):
+    """Channel pairs with one value of K and opposite values of q: thousands of nats of products, of which nothing is left but the last
+    group's ordinary logits.  Beside that of the result's type the error is that of fp32 sums: some 2^-23 of 15 scales times q, 10^-3 nats."""
+    rng = np.random.default_rng(d + group)
+    n = 400
+    k = np.repeat(rng.standard_normal((2, 1, n, d // 2)), 2, -1)
+    q = np.empty((2, n_q, group, d))
+    q[..., 0::2] = 1000 * rng.standard_normal((2, n_q, group, d // 2))
+    q[..., 1::2] = -q[..., 0::2]
+    q[..., -32:] = rng.standard_normal((2, n_q, group, 32))
+    c = Case(rng, [n, n], heads=1, d=d, k=k, v=rng.standard_normal((2, 1, n, d)))
+    q = torch.from_numpy(q).cuda().bfloat16()
+    out, code = c.attend(q, causal=False)
+    want, _ = bounds(c, q, False)
+    rounding = np.linalg.norm(pages.to_bf16(want) - want)
+    assert code == [0, 0] and np.linalg.norm(f64(out) - want) <= 1.15 * rounding, np.linalg.norm(f64(out) - want) / rounding
+
+
+@pytest.mark.parametrize("group,n_q", ROWS)
+def test_keys_of_the_largest_numbers_there_are(group, n_q):
+    """Keys of 10^37 and queries of 10^-33: logits of some 10^4, so that nearly all of a row's share is one key's."""
+    rng = np.random.default_rng(6)
+    v = rng.standard_normal((2, 1, 200, 128))
+    c = Case(rng, [200, 7], heads=1, k=2e37 * rng.standard_normal(v.shape).clip(-3, 3), v=v)
+    q = queries(rng, 2, n_q, group, 128, 1e-33)
+    got = f64(c.check(q, causal=False))
+    k, v = pages.values(c.ck, c.sk, c.zk)[:, 0], pages.values(c.cv, c.sv, c.zv)[:, 0]
+    x = np.einsum("bthd,bjd->bthj", f64(q), k) * 128 ** -0.5
+    x[1, ..., 7:] = -np.inf
+    best = np.sort(x, -1)
+    sure = best[..., -1] - best[..., -2] > 1e-3 * np.abs(best[..., -1])      # (what fp32 sums tell apart, and tens of nats)
+    want = np.stack([v[b][x[b].argmax(-1)] for b in range(2)])
+    tol = BF16 * np.abs(want) + FP16 * (np.abs(c.zv).max() + 8 * c.sv.max())
+    assert sure.any() and (np.abs(got - want) <= tol)[sure].all()
