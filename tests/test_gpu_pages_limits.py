@@ -3,9 +3,10 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import pages
 from paper_2411_10803_b200 import binding as md
 from paper_2411_10803_b200 import build as md_build
-from test_gpu_pages import Case, i32, queries, status, workspace
+from test_gpu_pages import Case, f64, i32, queries, status, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -156,3 +157,27 @@ def test_a_status_that_was_cleared_does_not_hide_the_next():
     cache.workspace[:1024] = 255                       # what a call that timed out may leave: a status and counters
     assert cache.device_status(clear=True)[0] != 0
     assert torch.equal(out, cache.attend(q)) and cache.device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("group,n_q", [(1, 1), (4, 1)])
+def test_the_longest_sequence_there_can_be(group, n_q):
+    """2^30 - 5 tokens over eight pages that the table names again and again: the attention over those pages' 1024 tokens.  Beside the result
+    type's half step, a warp's sums are cut at each of its 38 thousand chunks, by 2^-23 at most and half of that on average: 5e-3 of the values."""
+    rng = np.random.default_rng(group)
+    d, page, n_pages, length = 64, 128, 8, 2 ** 30 - 5
+    sizes = dict(n_seq=1, n_heads=1, head_dim=d, page=page, n_pages=n_pages)
+    k, v = queries(rng, 1, 1, 1024, d), queries(rng, 1, 1, 1024, d)
+    store = md.PageConfig(rows=1024, **sizes)
+    pool = torch.empty(md.mustdrop_page_pool_bytes(store), dtype=torch.uint8, device="cuda")
+    assert md.mustdrop_page_store(store, i32(np.arange(1024))[None], k, v, pool) == md.MUSTDROP_OK
+    cfg = md.PageConfig(q_heads=group, n_q=n_q, max_pages=2 ** 23, **sizes)
+    table = torch.arange(2 ** 23, dtype=torch.int32, device="cuda") % n_pages
+    q, ws = queries(rng, 1, n_q, group, d), workspace(cfg)
+    out = torch.zeros_like(q)
+    assert md.mustdrop_page_attend(cfg, q, pool, table, i32([length]), out, ws) == md.MUSTDROP_OK
+    assert status(ws) == [0, 0]
+    kk, vv = (pages.values(*pages.quantise(f64(x)))[0, 0] for x in (k, v))
+    x = f64(q)[0, 0] @ kk.T * d ** -0.5
+    p = np.exp(x - x.max(-1, keepdims=True))
+    p /= p.sum(-1, keepdims=True)
+    assert (np.abs(f64(out)[0, 0] - p @ vv) <= 2.0 ** -8 * np.abs(p @ vv) + 5e-3 * (p @ np.abs(vv)) + 2.0 ** -11 * np.abs(vv).max()).all()
