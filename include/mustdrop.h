@@ -370,7 +370,8 @@ mustdrop_status_t mustdrop_key_set(int32_t batch, int32_t n_heads, int32_t head_
  * z, both bf16, and 4-bit codes c; a value is z + s (c - 8).  With m, M the group's least and
  * greatest member: s = bf16((M/2 - m/2) / 7.5), z = bf16(m + 8 s), c = clamp(round((x - z) / s) + 8,
  * 0, 15), each step one fp32 operation, ties to even; c = 8 where s = 0.  A group with an infinity
- * or a NaN reads back as NaN.  (A value is off by at most s / 2, and by what rounding s and z moves.)
+ * or a NaN reads back as NaN.  (A value is off by at most s / 2, and by what rounding s and z moves; one beside the type's largest number
+ * may read back as an infinity.)
  *
  * Pool: n_pages x n_heads x (page / 16) chunks of 20 * head_dim bytes.  A chunk holds 16 tokens;
  * token k of it has the row r(k) = k / 2 + 8 (k mod 2).  With G = head_dim / 32, bytes in this order:
@@ -405,7 +406,7 @@ typedef struct {
   int32_t n_q;        /* attend: query tokens per sequence, 1..128 */
   int32_t causal;     /* attend: 1: query token t sees keys 0 .. len - n_q + t (the queries are the last n_q tokens); 0: all len keys */
   float   scale;      /* attend: logit scale, 0 .. 1e37; 0 => 1/sqrt(head_dim) */
-  int32_t flags;      /* 0 (or the debugging bit below) */
+  int32_t flags;      /* 0, or MUSTDROP_PAGE_FLAG_DEBUG_TIMEOUT */
   /* Strides in ELEMENTS (bf16); 0 => contiguous; each a multiple of 8.  Rows of head_dim elements are contiguous. */
   int64_t k_stride_s, k_stride_h, k_stride_r;   /* store: k [n_seq, n_heads, rows, head_dim] */
   int64_t v_stride_s, v_stride_h, v_stride_r;   /* store: v, likewise */
@@ -431,7 +432,9 @@ size_t mustdrop_page_workspace_bytes(const mustdrop_page_config_t *config /* (ho
  * count and can be taken by the NEXT call.  A sequence grows completely or not at all: it grows if it needs no new page, or if
  * the pages it and all sequences before it ask for (refused ones included) are free; otherwise its length stays
  * and MUSTDROP_ERR_NO_PAGES is recorded.  add[s] > rows, len[s] outside [0, max_pages * page] or growth beyond it:
- * the sequence stays as it is, MUSTDROP_ERR_BAD_LENGTH is recorded.
+ * the sequence stays as it is, MUSTDROP_ERR_BAD_LENGTH is recorded.  An id outside the pool that the table or the ring holds is passed on as it
+ * is and gives no slot (MUSTDROP_ERR_BAD_PAGE).  Every part of a call reads the lengths of all sequences before its own: calls of tens of
+ * thousands of sequences with thousands of rows each are not what it is made for (65535 x 4096: 3.8 ms).
  * Uses n_seq, page, n_pages, max_pages, rows of the configuration.
  */
 mustdrop_status_t mustdrop_page_tables(const mustdrop_page_config_t *config /* (host) */, const int32_t *add,

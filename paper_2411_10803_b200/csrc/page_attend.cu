@@ -16,8 +16,10 @@
 // instruction as two of fp16 behind conversions.)
 //
 // Bound: HBM where the issue slots keep up: a token and head is 1.25 D bytes where bf16 has 4 D, ~23 bytes per clock and SM, and takes
-// some 250 instructions per 16 tokens with one or two query rows, 340 with up to eight.  64 requests of 200 to 1800 keys, 32 heads: 70 us,
-// 4.7 TB/s (6.3 TB/s while every SM is at work); 2 of 90 to 131 thousand keys, 8 heads of 4 query heads: 69 us, 4.1 TB/s.
+// some 275 instructions per 16 tokens with one or two query rows, 370 with up to eight.  64 requests of 200 to 1800 keys, 32 heads: 69 us,
+// 4.8 TB/s (6.6 TB/s between the first landed chunk and the median warp's last); 2 of 90 to 131 thousand keys, 8 heads of 4 query heads: 72 us,
+// 3.9 TB/s.  More query rows than 16 are tiles that each read and unpack all pages again: 16 sequences of 2048 keys with 128 rows 77 us, 15 times
+// the products' time.
 //
 // Every warp walks its own range of chunks (16 tokens of one head, 20 D contiguous bytes, one bulk copy each), two at a
 // time, through its own ring in shared memory, without a barrier between warps.  The chunks of all (sequence, head, row tile) units form one
@@ -1067,14 +1069,14 @@ __global__ void __launch_bounds__(32 * Body::kWarps, 1) page_attend_kernel(const
   if (carry == 0) return;
 
   // This CTA's part of the line: an equal one, except that
-  //   - where every unit can have a CTA of its own and no warp then gets six chunks more than with equal parts, it has: nothing is
+  //   - where every unit can have a CTA of its own and no warp then gets more than eight chunks more than with equal parts, it has: nothing is
   //     joined across CTAs (one request, 32 heads, 640 keys: 7.5 us against 12.3);
   //   - where every unit can have a whole number of CTAs and parts get at most 38 chunks longer by that (2 us), they have: a CTA then
   //     has a part of one unit only, and joins are one instead of two in a row.  (One request, 8 heads of 4 query heads, 8192 keys: 13.3 us
   //     against 17.7, 131072 keys: 46.1 against 48.4; one of 32 heads, 4096 keys: 12.6 against 14.7; what it cannot help pays up to 0.4 us.)  No warp gets less than a pair of chunks for it: more
   //     parts are only more to join (2 heads of 4, 3000 keys: 11.6 us; with two pairs at least 13.1).
   //   - where that makes parts at most 72 chunks longer (4 us), their ends move to the nearest unit's, for the same reason: a join across
-  //     CTAs takes 3 to 5 us.  With units of one length, or few of them to a part, a part is then a whole number of the longest; with many
+  //     CTAs takes 3 to 5 us.  (The nearest shape that loses by it would grow by 78 chunks.)  With units of one length, or few of them to a part, a part is then a whole number of the longest; with many
   //     of different lengths it is about half a unit longer.  (64 requests of 200 to 1800 keys, 32 heads: 69.2 against 72.8 us, 9 of 2048 keys:
   //     23.6 against 27.9, 6 of 700: 11.5 against 15.0; but 16 of 1000 to 4000: 55.5 against 49.7.)
   const long long total = static_cast<long long>(carry) * units_per_seq;

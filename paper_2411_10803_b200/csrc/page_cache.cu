@@ -39,8 +39,9 @@ namespace {
 // ring[head + count + P_back + i].  The ring's two ends never meet (count + all of back <= n_pages), so no CTA
 // waits for another: each sums need and back over the sequences before its own (two loads per sequence, from L2) and
 // handles its own ones.  What the others still read - lengths and state that are updated in place - is written by the CTA that finishes
-// last; one CTA alone, or outputs of their own, need no such order.  Bound: launch and three dependent trips to L2
-// (240 sequences, one token: 4.3 us), the slots written for large calls.
+// last, in a second walk over all of them; one CTA alone, or outputs of their own, need no such order.  Bound: launch and three dependent trips
+// to L2 (240 sequences, one token: 4.4 us), for many sequences the sums, which grow with their square, and the walk (2048 sequences, one token:
+// 6.4 us with outputs of their own, 10 in place; 65535: 21 and 117).
 struct TableParams {
   const int32_t *add, *len, *state;
   int32_t *len_out, *state_out, *ring, *table, *slots;
@@ -281,11 +282,11 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
 // group needs once - range, scale, centre, reciprocal - is computed once.  A word of the V codes holds four tokens, so lanes of
 // four neighbouring rows exchange theirs and store whole words where their slots are one word's, else single bytes; rows are
 // taken so that they are: fours end where slot mod 4 is 3, judged by the sequence's first slot.  With one row per sequence (decoded tokens) a
-// warp's rows are heads instead.  Bound: bytes for large calls (64 x 2048 x 8 rows, 705 MB: 123 us, 5.7 TB/s), also instructions for those of
-// 100 MB (32 x 192 x 32 one after the other: 26.5 us, 5.0 TB/s).
+// warp's rows are heads instead.  Bound: bytes for large calls (64 x 2048 x 8 rows, 705 MB: 123 us, 5.7 TB/s), for those of
+// 100 MB neither bytes nor issue alone (32 x 192 x 32 one after the other: 28 us, 4.7 TB/s, issue slots 64 %, ALU pipe 67 %, 39 % of the warps).
 //
 // Load: 16 lanes hold a row of 128 channels (8 of 64) as 16-byte vectors.  Bound: the bytes written (32 x 608 x 32 rows: 79 us, 4.0 TB/s; a
-// plain fill of as many bytes runs at 3.8).
+// plain fill of its buffers runs at 3.9).
 // Both: small CTAs, as warps that finish hold their place until the CTA's last one has (256 threads: store 2 to 7 %, load 3 % slower).  And
 // no early start of the call that follows: its CTAs would crowd onto the few SMs that are free by then and stay there (with one after 64
 // requests' attention, tables, store and attention of the next layer take 79 us, without 71; a store and a load of one token 9.4 against 7.9).
