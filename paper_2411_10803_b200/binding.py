@@ -565,8 +565,9 @@ class PagedCache:
         import torch
         if stream is None:
             return None
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
+        if not isinstance(stream, torch.cuda.Stream):        # a raw handle, or what holds one (as everywhere)
+            handle = _stream(stream)
+            stream = torch.cuda.ExternalStream(handle, device=self.device) if handle else torch.cuda.default_stream(self.device)
         return None if stream.cuda_stream == torch.cuda.current_stream(self.device).cuda_stream else stream
 
     def _empty(self, shape, dtype, stream):

@@ -69,12 +69,22 @@ def filled(n, heads=2, rows=40):
     return cache
 
 
-@pytest.mark.parametrize("raw", [False, True])
-def test_results_of_a_call_on_another_stream_are_not_handed_out_again(raw):
+class Held:
+    """A stream of another library: something with a raw handle."""
+
+    def __init__(self, stream):
+        self.cuda_stream = stream.cuda_stream
+
+
+KINDS = {"torch": lambda s: s, "raw": lambda s: s.cuda_stream, "held": Held}
+
+
+@pytest.mark.parametrize("kind", sorted(KINDS))
+def test_results_of_a_call_on_another_stream_are_not_handed_out_again(kind):
     cache = filled(64)
     q = queries(np.random.default_rng(1), 64, 1, 2, 128)
     side = torch.cuda.Stream()
-    on = side.cuda_stream if raw else side
+    on = KINDS[kind](side)
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
         torch.cuda._sleep(LONG)
